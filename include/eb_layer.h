@@ -412,6 +412,135 @@ eb_status eb_op_attention(eb_handle *h, const void *qkv, const eb_kv_cache *kv, 
 eb_status eb_op_gather_kv(eb_handle *h, const eb_kv_cache *kv, const eb_batch *batch, void *out_k,
                           void *out_v, void *ws, size_t ws_bytes, void *stream);
 
+/* ---- operators on the paged cache for models and services beyond the layer
+ * step above: other rotary positions, other scores and masks, and caches that
+ * are cut back to a budget.  Same conventions, with these additions:
+ *  - a call enqueues kernels only (request tables travel in their arguments),
+ *    so it can be captured into a graph; a replay repeats it with the lengths
+ *    it was captured with.  Calls and graphs that may run at the same time
+ *    need workspaces of their own.
+ *  - the current device must be the one the handle was created on
+ *    (EB_ERR_CONFIG otherwise), and the device pointers must be its own.
+ *  - activations, caches and workspaces are 16-byte aligned or better (as
+ *    allocators give them; EB_ERR_CONFIG otherwise). */
+
+/* How pairs of a head's dims turn with the position.  The first rotary_dim
+ * dims of each q and k head are rotated (a positive multiple of 16, at most
+ * head_dim; 0: head_dim), the others stay as they are.  With R = rotary_dim,
+ * pair t < R / 2 is dims (t, t + R / 2) for EB_ROTARY_HALF, (2t, 2t + 1) for
+ * EB_ROTARY_INTERLEAVED, and turns by position * f_t radians,
+ *   (x, y) -> magnitude * (x cos - y sin, x sin + y cos),
+ * where w_t = theta^(-2t/R) and
+ *   EB_ROTARY_PLAIN       f_t = w_t
+ *   EB_ROTARY_LINEAR      f_t = w_t / factor
+ *   EB_ROTARY_NTK         f_t = w_t of the base theta factor^(R / (R - 2))
+ *   EB_ROTARY_WAVELENGTH  by how often the pair turns in original_len
+ *                         positions, n_t = original_len w_t / 2 pi: w_t from
+ *                         high turns on, w_t / factor up to low turns, and
+ *                         between them the mix ((n_t - low) / (high - low))
+ *                         of the former with the rest of the latter
+ *   EB_ROTARY_YARN        w_t (1 - g_t) + (w_t / factor) g_t, the ramp g_t =
+ *                         clamp((t - a) / (b - a), 0, 1) running over the
+ *                         pair index from a = floor(i(high)) >= 0 to b =
+ *                         ceil(i(low)) <= R - 1 (b - a at least 1e-3), where
+ *                         i(n) = R ln(original_len / (2 pi n)) / (2 ln theta)
+ * (Peng et al., "YaRN", 2023, for the last).  factor >= 1, original_len >= 1
+ * and 0 < low < high where they are used; low and high of 0 mean 1 and 4
+ * (WAVELENGTH) or 1 and 32 (YARN).  magnitude 0 means 1, and for YARN
+ * 0.1 ln(factor) + 1.  theta > 1.  q_norm, k_norm: bf16 [head_dim] gains of the
+ * per-head RMSNorm before the rotation, required for a handle with qk_norm
+ * and ignored otherwise. */
+typedef enum eb_rotary_layout { EB_ROTARY_HALF = 0, EB_ROTARY_INTERLEAVED = 1 } eb_rotary_layout;
+typedef enum eb_rotary_scaling {
+  EB_ROTARY_PLAIN = 0,
+  EB_ROTARY_LINEAR = 1,
+  EB_ROTARY_NTK = 2,
+  EB_ROTARY_WAVELENGTH = 3,
+  EB_ROTARY_YARN = 4
+} eb_rotary_scaling;
+typedef struct eb_rotary {
+  int32_t rotary_dim, layout, scaling;
+  float theta, factor, low, high, magnitude;
+  int32_t original_len;
+  const void *q_norm, *k_norm;
+} eb_rotary;
+
+/* eb_op_rope_kv_append with the rotation described by rot.  positions: device
+ * int32 [num_tokens], the position of each row, which need not be its cache
+ * slot c_i + j (a cache that was cut back has fewer slots than positions);
+ * NULL: c_i + j.  Any int32 value is a position.  qkv's q heads are rotated in
+ * place; the rotated k and the v heads are stored at slots c_i + j, and k and v
+ * in qkv stay as they came.  kv NULL: no cache; the k heads are rotated in
+ * place too.  The angle is reduced in 64 bits, so far positions lose nothing.
+ * A block-table id outside the pool stores nothing. */
+size_t eb_op_rotary_kv_append_workspace_bytes(const eb_handle *h, const eb_batch *batch);
+eb_status eb_op_rotary_kv_append(eb_handle *h, const eb_rotary *rot, void *qkv, const eb_kv_cache *kv,
+                                 const eb_batch *batch, const int32_t *positions, void *ws, size_t ws_bytes,
+                                 void *stream);
+
+/* Scores and masks of eb_op_attention_mod.  For the row at cache position p =
+ * c_i + j of request i and the key at position t of the same request:
+ *   s = scale * q.k                         (scale 0: 1 / sqrt(head_dim); else finite, > 0)
+ *   s = softcap * tanh(s / softcap)         when softcap > 0 (at most 1000)
+ *   s = s - slopes[head] * |p - t|          when slopes (device fp32 [n_q]) is given
+ * and the key is visible iff
+ *   max(first_key[row], p - window + 1, 0) <= t < max(p + 1, prefix_lens_host[i]).
+ * window 0: none.  first_key: device int32 [num_tokens] or NULL, the first key
+ * a row may see (of its document in a packed sequence; past p for a padding
+ * row, which then sees nothing).  prefix_lens_host: HOST int32 [num_seqs] or
+ * NULL; keys before it are visible to every row of the request, later ones
+ * included (0 <= prefix <= c_i + n_i, EB_ERR_BATCH otherwise).  A zeroed struct, or NULL, is
+ * causal attention.  Distances count cache positions. */
+typedef struct eb_score_mod {
+  float scale, softcap;
+  const float *slopes;
+  int32_t window;
+  const int32_t *prefix_lens_host, *first_key;
+} eb_score_mod;
+
+/* Attention of every row over the visible keys of its request, as
+ * eb_op_attention with the scores and masks of mod; decode rows, chunks and
+ * both together.  Keys and values that a row does not see do not reach it, not
+ * even as infinities or NaN; pages that no row sees are not read.  A row that
+ * sees nothing gets zeros.
+ * lse (fp32 [num_tokens, n_q] or NULL): ln of the sum of exp(s) over the
+ * visible keys, -inf for a row that sees nothing.
+ * kv_weights (or NULL): the weight each cached key has received, fp32
+ * [num_pages, n_kv_heads, page_size], paged as the cache is.  The call adds to
+ * every cached key the softmax weights of the rows and of the heads of its
+ * group; the keys of the new rows start at what this call gives them; other
+ * slots keep theirs.  weight_rows > 0: only the last weight_rows rows of each
+ * request count.  No atomics: the same call gives the same bits.
+ * want_weights: whether kv_weights will be given. */
+size_t eb_op_attention_mod_workspace_bytes(const eb_handle *h, const eb_batch *batch, const eb_score_mod *mod,
+                                           int32_t want_weights);
+eb_status eb_op_attention_mod(eb_handle *h, const void *qkv, const eb_kv_cache *kv, const eb_batch *batch,
+                              const eb_score_mod *mod, void *out, float *lse, float *kv_weights,
+                              int32_t weight_rows, void *ws, size_t ws_bytes, void *stream);
+
+/* Cuts caches back to a budget by the weight their keys received.  Request i
+ * holds lens_host[i] keys (>= 0) in the pages of src and keeps k_i =
+ * min(keep_lens_host[i], lens_host[i]) of them per kv head: the first `sink`,
+ * the last `recent`, and of the rest those of the largest kv_weights (equal
+ * ones: the lower position; NaN counts as largest, both zeros as equal).
+ * sink + recent must fit: min(lens, sink + recent) <= keep_lens (EB_ERR_BATCH).
+ * The kept keys, values and (dst_weights not NULL) weights are copied in
+ * order of position to slots 0 .. k_i - 1 of dst's pages; nothing else of dst
+ * is written.  The kv heads choose apart, so a slot holds other positions'
+ * keys in each; rotated keys keep their rotation.  src and dst may be the same
+ * cache arrays with other block tables (the old pages, which other requests
+ * may share, stay as they are), but no destination page may be a source page.
+ * Element types must agree, 8-bit scales too (EB_ERR_CONFIG).
+ * kept (device int32 [num_seqs, n_kv_heads, kept_stride], kept_stride >= the
+ * largest k_i, or NULL): the kept positions, ascending; entries past k_i are
+ * left as they were. */
+size_t eb_op_kv_evict_workspace_bytes(const eb_handle *h, int32_t num_seqs, const int32_t *lens_host,
+                                      const int32_t *keep_lens_host);
+eb_status eb_op_kv_evict(eb_handle *h, const eb_kv_cache *src, const float *kv_weights, int32_t num_seqs,
+                         const int32_t *lens_host, const int32_t *keep_lens_host, int32_t sink, int32_t recent,
+                         const eb_kv_cache *dst, float *dst_weights, int32_t *kept, int32_t kept_stride, void *ws,
+                         size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,7 +30,9 @@ SYMBOLS = ("eb_create", "eb_destroy", "eb_workspace_bytes", "eb_layer_step_decod
            "eb_op_gemm_workspace_bytes", "eb_op_gemm", "eb_op_gemm_w8", "eb_op_moe_ffn_workspace_bytes", "eb_op_moe_ffn", "eb_op_rope_kv_append", "eb_op_attention",
            "eb_op_gather_kv", "eb_profile", "eb_profile_read", "eb_profile_stage_name", "eb_stack_workspace_bytes",
            "eb_stack_step", "eb_workspace_offset", "eb_noalloc_scratch_bytes", "eb_layer_step_mixed_noalloc",
-           "eb_packed_weight_bytes", "eb_pack_weight")
+           "eb_packed_weight_bytes", "eb_pack_weight", "eb_op_rotary_kv_append_workspace_bytes",
+           "eb_op_rotary_kv_append", "eb_op_attention_mod_workspace_bytes", "eb_op_attention_mod",
+           "eb_op_kv_evict_workspace_bytes", "eb_op_kv_evict")
 
 
 class EbError(RuntimeError):
@@ -72,6 +74,22 @@ class Batch(ctypes.Structure):
                 ("context_lens_host", ctypes.c_void_p), ("chunk_lens_host", ctypes.c_void_p)]
 
 
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "wavelength": 3, "yarn": 4}
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("theta", ctypes.c_float), ("factor", ctypes.c_float), ("low", ctypes.c_float),
+                ("high", ctypes.c_float), ("magnitude", ctypes.c_float), ("original_len", ctypes.c_int32),
+                ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p)]
+
+
+class ScoreMod(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+                ("window", ctypes.c_int32), ("prefix_lens_host", ctypes.c_void_p), ("first_key", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -105,6 +123,12 @@ def lib() -> ctypes.CDLL:
         "eb_op_rope_kv_append": (I32, [VP, VP, P(KvCache), P(Batch), VP, SZ, VP]),
         "eb_op_attention": (I32, [VP, VP, P(KvCache), P(Batch), VP, VP, SZ, I32, VP]),
         "eb_op_gather_kv": (I32, [VP, P(KvCache), P(Batch), VP, VP, VP, SZ, VP]),
+        "eb_op_rotary_kv_append_workspace_bytes": (SZ, [VP, P(Batch)]),
+        "eb_op_rotary_kv_append": (I32, [VP, P(Rotary), VP, P(KvCache), P(Batch), VP, VP, SZ, VP]),
+        "eb_op_attention_mod_workspace_bytes": (SZ, [VP, P(Batch), P(ScoreMod), I32]),
+        "eb_op_attention_mod": (I32, [VP, VP, P(KvCache), P(Batch), P(ScoreMod), VP, VP, VP, I32, VP, SZ, VP]),
+        "eb_op_kv_evict_workspace_bytes": (SZ, [VP, I32, VP, VP]),
+        "eb_op_kv_evict": (I32, [VP, P(KvCache), VP, I32, VP, VP, I32, I32, P(KvCache), VP, VP, I32, VP, SZ, VP]),
         "eb_profile": (I32, [VP, I32, ctypes.c_uint32]),
         "eb_profile_read": (I32, [VP, P(ctypes.c_float), I32]),
         "eb_profile_stage_name": (ctypes.c_char_p, [I32]),
@@ -486,6 +510,156 @@ def eb_op_gather_kv(h: Handle, k_cache, v_cache, block_tables, context_lens, chu
     _check(lib().eb_op_gather_kv(h.h, ctypes.byref(kv), ctypes.byref(hb.c), _ptr(ok), _ptr(ov), _ptr(ws), ws.numel(),
                                  _stream(stream)))
     return ok, ov
+
+
+# ---------------------------------------------------------------------------
+# operators on the paged cache: rotary append, modified attention, eviction.
+# They take the structs that a program keeps between calls: kv_struct(..) of
+# its cache and HostBatch(..) of the request lengths.  Structs made here hold
+# on to the tensors they point to; a kv_struct's cache and tables are the
+# caller's to keep.
+# ---------------------------------------------------------------------------
+
+def _dev(t: torch.Tensor, dtype, name: str, numel: Optional[int] = None):
+    """Device address of a contiguous GPU tensor of this dtype (and size)."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name} must have {numel} elements")
+    return t.data_ptr()
+
+
+def _lens(a, name: str) -> np.ndarray:
+    a = np.asarray(a)
+    if a.dtype == np.int32 and a.flags.c_contiguous and a.ndim == 1:
+        return a
+    if a.ndim != 1 or (a.size and not np.issubdtype(a.dtype, np.integer)):
+        raise TypeError(f"{name} must be a 1-D array of integers")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def _ws(ws: Optional[torch.Tensor], nbytes, stream):
+    """(tensor to keep alive, address, bytes) of a workspace; allocated when None."""
+    if ws is None:
+        ws = alloc_workspace(nbytes())
+        if stream is not None:  # its memory is not given out again before that stream is done with it
+            ws.record_stream(stream)
+    return ws, _dev(ws, torch.uint8, "ws"), ws.numel()
+
+
+def rotary(theta: float, rotary_dim: int = 0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+           original_len: int = 0, low: float = 0.0, high: float = 0.0, magnitude: float = 0.0,
+           q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None) -> Rotary:
+    """The rotation of eb_op_rotary_kv_append (eb_rotary); zeros stand for
+    the defaults the header gives."""
+    r = Rotary(int(rotary_dim), ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], float(theta), float(factor),
+               float(low), float(high), float(magnitude), int(original_len),
+               None if q_norm is None else _dev(q_norm, torch.bfloat16, "q_norm"),
+               None if k_norm is None else _dev(k_norm, torch.bfloat16, "k_norm"))
+    r.held = (q_norm, k_norm)
+    return r
+
+
+def eb_op_rotary_kv_append_workspace_bytes(h: Handle, batch: HostBatch) -> int:
+    return int(lib().eb_op_rotary_kv_append_workspace_bytes(h.h, ctypes.byref(batch.c)))
+
+
+def eb_op_rotary_kv_append(h: Handle, rot: Rotary, qkv: torch.Tensor, kv: Optional[KvCache], batch: HostBatch,
+                           positions: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Rotates the q heads of qkv in place and stores rotated k and v in the
+    cache (kv None: rotates k in place too); returns qkv."""
+    T, s = batch.c.num_tokens, h.cfg
+    p = _dev(qkv, torch.bfloat16, "qkv", T * (s.n_q_heads + 2 * s.n_kv_heads) * s.head_dim)
+    pos = None if positions is None else _dev(positions, torch.int32, "positions", T)
+    held, wp, wn = _ws(ws, lambda: eb_op_rotary_kv_append_workspace_bytes(h, batch), stream)
+    _check(lib().eb_op_rotary_kv_append(h.h, ctypes.byref(rot), p, None if kv is None else ctypes.byref(kv),
+                                        ctypes.byref(batch.c), pos, wp, wn, _stream(stream)))
+    return qkv
+
+
+def score_mod(scale: float = 0.0, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, window: int = 0,
+              first_key: Optional[torch.Tensor] = None, prefix_lens=None) -> ScoreMod:
+    """Scores and masks of eb_op_attention_mod (eb_score_mod)."""
+    pre = None if prefix_lens is None else _lens(prefix_lens, "prefix_lens")
+    m = ScoreMod(float(scale), float(softcap), None if slopes is None else _dev(slopes, torch.float32, "slopes"),
+                 int(window), None if pre is None else pre.ctypes.data,
+                 None if first_key is None else _dev(first_key, torch.int32, "first_key"))
+    m.held = (slopes, first_key, pre)
+    return m
+
+
+def _check_mod(h: Handle, batch: HostBatch, m: Optional[ScoreMod]):
+    slopes, first, pre = m.held if m is not None else (None, None, None)
+    if slopes is not None and slopes.numel() != h.cfg.n_q_heads:
+        raise ValueError("slopes needs one value per query head")
+    if first is not None and first.numel() != batch.c.num_tokens:
+        raise ValueError("first_key needs one value per row")
+    if pre is not None and len(pre) != batch.c.num_seqs:
+        raise ValueError("prefix_lens needs one value per request")
+    return None if m is None else ctypes.byref(m)
+
+
+def eb_op_attention_mod_workspace_bytes(h: Handle, batch: HostBatch, mod: Optional[ScoreMod] = None,
+                                        want_weights: bool = False) -> int:
+    return int(lib().eb_op_attention_mod_workspace_bytes(h.h, ctypes.byref(batch.c), _check_mod(h, batch, mod),
+                                                         1 if want_weights else 0))
+
+
+def eb_op_attention_mod(h: Handle, qkv: torch.Tensor, kv: KvCache, batch: HostBatch, mod: Optional[ScoreMod] = None,
+                        out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                        kv_weights: Optional[torch.Tensor] = None, weight_rows: int = 0,
+                        ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention with modified scores and masks; out bf16 [T, n_q head_dim],
+    lse fp32 [T, n_q] and kv_weights fp32 [pages, n_kv, 16] where wanted."""
+    T, s = batch.c.num_tokens, h.cfg
+    p = _dev(qkv, torch.bfloat16, "qkv", T * (s.n_q_heads + 2 * s.n_kv_heads) * s.head_dim)
+    if out is None:
+        out = torch.empty(T, s.n_q_heads * s.head_dim, dtype=torch.bfloat16, device=qkv.device)
+        if stream is not None:
+            out.record_stream(stream)
+    o = _dev(out, torch.bfloat16, "out", T * s.n_q_heads * s.head_dim)
+    z = None if lse is None else _dev(lse, torch.float32, "lse", T * s.n_q_heads)
+    w = None if kv_weights is None else _dev(kv_weights, torch.float32, "kv_weights",
+                                             kv.num_pages * s.n_kv_heads * s.page_size)
+    m = _check_mod(h, batch, mod)
+    held, wp, wn = _ws(ws, lambda: eb_op_attention_mod_workspace_bytes(h, batch, mod, w is not None), stream)
+    _check(lib().eb_op_attention_mod(h.h, p, ctypes.byref(kv), ctypes.byref(batch.c), m, o, z, w, int(weight_rows),
+                                     wp, wn, _stream(stream)))
+    return out
+
+
+def eb_op_kv_evict_workspace_bytes(h: Handle, lens, keep_lens) -> int:
+    a, b = _lens(lens, "lens"), _lens(keep_lens, "keep_lens")
+    if len(a) != len(b):
+        raise ValueError("lens and keep_lens need one value per request each")
+    return int(lib().eb_op_kv_evict_workspace_bytes(h.h, len(a), a.ctypes.data, b.ctypes.data))
+
+
+def eb_op_kv_evict(h: Handle, src: KvCache, kv_weights: torch.Tensor, lens, keep_lens, dst: KvCache,
+                   dst_weights: Optional[torch.Tensor] = None, sink: int = 0, recent: int = 0,
+                   kept: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> np.ndarray:
+    """Copies the keys to keep from src's pages to dst's; returns the requests'
+    new lengths.  kept: int32 [requests, n_kv, >= the largest of them]."""
+    a, b = _lens(lens, "lens"), _lens(keep_lens, "keep_lens")
+    if len(a) != len(b):
+        raise ValueError("lens and keep_lens need one value per request each")
+    s = h.cfg
+    w = _dev(kv_weights, torch.float32, "kv_weights", src.num_pages * s.n_kv_heads * s.page_size)
+    d = None if dst_weights is None else _dev(dst_weights, torch.float32, "dst_weights",
+                                              dst.num_pages * s.n_kv_heads * s.page_size)
+    k, stride = None, 0
+    if kept is not None:
+        if kept.dim() != 3 or kept.shape[0] != len(a) or kept.shape[1] != s.n_kv_heads:
+            raise ValueError("kept must be [requests, n_kv, keys]")
+        k, stride = _dev(kept, torch.int32, "kept"), kept.shape[2]
+    held, wp, wn = _ws(ws, lambda: eb_op_kv_evict_workspace_bytes(h, a, b), stream)
+    _check(lib().eb_op_kv_evict(h.h, ctypes.byref(src), w, len(a), a.ctypes.data, b.ctypes.data, int(sink),
+                                int(recent), ctypes.byref(dst), d, k, int(stride), wp, wn, _stream(stream)))
+    return np.minimum(a, b)
 
 
 def eb_profile(h: Handle, enable: bool = True, steps: int = 1, stages=None):

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/eb_layer.h"
+#include "api_internal.h"
 #include "eb_internal.h"
 #include "host_plan.h"
 
@@ -604,6 +605,21 @@ eb_status run_layers(eb_handle *h, int32_t n_layers, const eb_layer_weights *w, 
 }
 
 }  // namespace
+
+namespace eb {
+eb_status api_fail(eb_status s, const std::string &msg) { return fail(s, msg); }
+eb_status api_hip_fail(hipError_t e, const char *what) { return hip_fail(e, what); }
+eb_status api_check_kv(const eb_kv_cache *kv) { return check_kv(kv); }
+eb_status api_check_ws(void *ws, size_t ws_bytes, size_t need) { return check_ws(ws, ws_bytes, need); }
+eb_status api_check_batch(const eb_handle *h, const eb_batch *b, int32_t max_pages) {
+  return check_common(h, b, EB_MODE_MIXED, max_pages);
+}
+eb_status api_debug_tables(const eb_handle *h, const eb_batch *b, const eb_kv_cache *kv, hipStream_t st) {
+  return debug_check_tables(h, b, kv, 1, st);
+}
+KV api_kv(const eb_kv_cache *kv) { return kv_of(kv); }
+HandleView api_view(const eb_handle *h) { return HandleView{&h->cfg, &h->shape, h->max_seqs, h->device, h->debug_validate}; }
+}  // namespace eb
 
 extern "C" {
 

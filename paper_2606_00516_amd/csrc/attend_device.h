@@ -1,0 +1,105 @@
+// What the kernels of the modified attention share: their arguments, the
+// score of a key and the rows' visible ranges.
+//
+//   s = scale q.k;  s = cap tanh(s / cap) with a cap;  s -= slope |p - t| with
+//   a distance bias;  key t is visible to the row at position p iff
+//   max(first_key, p - window + 1, 0) <= t < max(p + 1, prefix).
+// Scores are held in log2 units.
+#pragma once
+#include "attention_tiles.h"
+#include "op_meta.h"
+#include "ops.h"
+
+namespace eb {
+
+constexpr float kNoScore = -__builtin_inff();
+
+struct AttendArgs {
+  const uint16_t *qkv;
+  uint16_t *out;
+  float *lse, *weights, *part_o, *part_ml, *scores;
+  const int32_t *first_key;
+  const float *slopes;
+  KV kv;
+  int32_t nq, nkv, group, window, n, weight_rows;  // n: requests of the table
+  float qscale;                                    // no cap: to log2 units; cap: 2 log2(e) scale / cap
+  float cap2;                                      // cap in log2 units
+  const int32_t *meta;
+  Words inl;
+};
+static_assert(sizeof(AttendArgs) < 4096, "kernel arguments");
+
+// One score from its raw product.  tanh(x) = 1 - 2 / (e^2x + 1), exact at
+// both ends (e^2x = 0 and infinite); its error of an ulp of 1 is below 1e-5
+// of a probability for caps of 100 and less.
+template <bool CAP>
+EB_DEV float mod_score(float raw, float qscale, float cap2) {
+  if constexpr (!CAP) return raw * qscale;
+  const float e = fast_exp2(raw * qscale);
+  return fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(e + 1.0f), cap2);
+}
+
+// First key the row at position p may see (the window and its own bound).
+EB_DEV int row_first(const AttendArgs &a, int row, int p) {
+  int lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
+  if (a.first_key) lo = max(lo, a.first_key[row]);
+  return lo;
+}
+
+// Waits until at most N of the wavefront's vector memory operations are
+// outstanding.  The direct loads into LDS are waited for by name: the
+// compiler's own count has been seen to leave one out where a loop carries
+// them over its back edge.
+template <int N>
+EB_DEV void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
+}
+
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// Joins ns partials (entries base, base + nq, ..) into row entry `at` of out
+// and lse, by one wavefront: lane s % 64 holds partial s's factor, HD / 64 output
+// dims per lane, eight partials' loads issued together.
+template <int HD>
+EB_DEV void join_splits(const AttendArgs &a, size_t base, int ns, size_t at, bool empty, int lane) {
+  constexpr int DPL = HD / 64;
+  const size_t stride = (size_t)a.nq;
+  float mx = kNoScore;
+  for (int s = lane; s < ns; s += 64) mx = fmaxf(mx, a.part_ml[(base + s * stride) * 2]);
+  mx = wave_max(mx);
+  float den = 0.f, acc[DPL];
+#pragma unroll
+  for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
+  for (int c = 0; c < ns; c += 64) {
+    const int s = c + lane;
+    float f = 0.f;
+    if (s < ns) {
+      const float ms = a.part_ml[(base + s * stride) * 2];
+      f = ms == kNoScore ? 0.f : fast_exp2(ms - mx);
+      if (f != 0.f) den += f * a.part_ml[(base + s * stride) * 2 + 1];
+    }
+    const int n = min(64, ns - c);
+    for (int j = 0; j < n; j += 8) {
+      float o[8][DPL];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int i = 0; i < DPL; ++i)
+          o[u][i] = j + u < n ? a.part_o[(base + (size_t)(c + j + u) * stride) * HD + lane * DPL + i] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j + u));
+        // (a split that saw nothing wrote no outputs)
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) acc[i] = w != 0.f ? fmaf(w, o[u][i], acc[i]) : acc[i];
+      }
+    }
+  }
+  den = wave_sum(den);
+#pragma unroll
+  for (int i = 0; i < DPL; ++i)
+    a.out[at * HD + lane * DPL + i] = (uint16_t)f32_to_bf16_bits(empty ? 0.f : acc[i] / den);
+  if (lane == 0 && a.lse) a.lse[at] = empty ? kNoScore : kLn2 * (mx + log2f(den));
+}
+
+}  // namespace eb

@@ -128,6 +128,16 @@ EB_DEV uint32_t e4m3x4_from_f32(float a, float b, float c, float d) {
   return w;
 }
 
+// Codes of eight bf16 values (packed pairs) divided by scale.
+EB_DEV u32x2_t e4m3x8_of_bf16x8(u32x4_t w, float scale) {
+  u32x2_t r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    r[i] = e4m3x4_from_f32(bf16_lo(w[2 * i]) / scale, bf16_hi(w[2 * i]) / scale, bf16_lo(w[2 * i + 1]) / scale,
+                           bf16_hi(w[2 * i + 1]) / scale);
+  return r;
+}
+
 // D = A B + C on one 16x16x32 bf16 tile.  Operand layout (lane l):
 //   A: row l % 16, k = 8 (l / 16) .. + 7      B: col l % 16, same k
 //   C/D: rows 4 (l / 16) .. + 3, col l % 16

@@ -1,0 +1,502 @@
+// Rows of requests with several new rows (prompt chunks, drafted tokens) in
+// the modified attention.
+//
+// A block takes 128 query rows (128 / G positions of the G heads of one kv
+// head) of one request and a range of its keys, in tiles of 64.  Four
+// wavefronts hold 32 rows each: S^T = K Q^T and O^T += V^T P^T on 32x32x16
+// products, so a row's scores lie in one lane pair, its softmax needs one
+// exchange, and P goes from the score registers straight into the second
+// product.  Two LDS buffers of a K and a V tile (row-major, swizzled) are
+// filled by direct loads, K two tiles and V one tile ahead, so the scores of
+// tile t + 1 run on the matrix cores under the exponentials of tile t; 8-bit
+// tiles pass through registers to become bf16.  Per tile and wavefront 32
+// products of 32 cycles stand against 32 scores per lane: about 28 cycles of
+// vector work each, 70 with the cap (two more transcendentals of 16 cycles),
+// which makes capped attention bound by the vector unit.
+//
+// With few rows the keys are split over blocks (the plan's rule) and joined by
+// k_attend_chunk_combine.
+#include "attend_device.h"
+
+#include <type_traits>
+
+namespace eb {
+
+namespace {
+
+constexpr int kWaves = 4;
+// The running maximum moves only when a tile exceeds it by more than this
+// (log2 units): probabilities stay below 2^8, exact alike in fp32 and bf16,
+// and most tiles skip the rescaling of the outputs.
+constexpr float kSlack = 8.0f;
+
+struct PreReq {
+  int k, seq, row0, c, n, prefix, nsplit;
+};
+__device__ __forceinline__ PreReq pre_req(const AttendArgs &a, const int32_t *m, int k) {
+  PreReq r;
+  r.k = k;
+  // (uniform; said so, so that what follows from them stays in scalar registers)
+  r.seq = __builtin_amdgcn_readfirstlane(m[PRE_SEQ * a.n + k]);
+  r.row0 = __builtin_amdgcn_readfirstlane(m[PRE_ROW * a.n + k]);
+  r.c = __builtin_amdgcn_readfirstlane(m[PRE_CTX * a.n + k]);
+  r.n = __builtin_amdgcn_readfirstlane(m[PRE_LEN * a.n + k]);
+  r.prefix = __builtin_amdgcn_readfirstlane(m[PRE_PREFIX * a.n + k]);
+  r.nsplit = __builtin_amdgcn_readfirstlane(m[PRE_NSPLIT * a.n + k]);
+  return r;
+}
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+template <int HD, bool F8, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
+  constexpr int KT = kAttendTile;
+  constexpr int ROW = HD * 2;        // bytes per key row in LDS
+  constexpr int CPR = ROW / 16;      // 16-byte chunks per row
+  constexpr int TILE = KT * ROW;     // bytes of the K (and of the V) tile
+  constexpr int NKS = HD / 16;       // k-steps of the score product
+  constexpr int NOB = HD / 32;       // 32-dim output blocks
+  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE];
+  __shared__ int red[2], odd[2];
+  uint8_t *const buf0 = lds, *const buf1 = lds + 2 * TILE;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, lh = lane >> 5;
+  const int32_t *m = meta_words(a);
+  const int tile_id = blockIdx.x / a.nkv, kh = blockIdx.x - tile_id * a.nkv;
+  const PreReq r = pre_req(a, m, last_at_or_below(m + PRE_TILE0 * a.n, a.n, tile_id));
+  const int G = a.group, BQ = kAttendRows / G;
+  const int nqb = (r.n + BQ - 1) / BQ;
+  const int local = __builtin_amdgcn_readfirstlane(tile_id - m[PRE_TILE0 * a.n + r.k]);
+  // the last rows, which see the most keys, first
+  const int qb = nqb - 1 - local / r.nsplit, sp = local % r.nsplit;
+  const int q_lo = qb * BQ, q_hi = min(r.n, q_lo + BQ);
+  const int klen = r.c + r.n;
+  const int cols = (a.nq + 2 * a.nkv) * HD;
+
+  // this lane's row: 32 rows of a wave are RPH positions of 32 / RPH heads
+  const int RPH = min(BQ, 32), HG = G * RPH / 32;
+  const int hb = wave % HG, sub = wave / HG;
+  const int hrow = hb * (32 / RPH) + lq / RPH;
+  const int qrel = q_lo + sub * RPH + lq % RPH;
+  const bool qok = qrel < q_hi;
+  const int qpos = r.c + qrel;
+  u32x4_t qreg[NKS];
+  {
+    const uint16_t *src = a.qkv + (size_t)(r.row0 + (qok ? qrel : 0)) * cols + (kh * G + hrow) * HD + lh * 8;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      const u32x4_t v = ld_u32x4(src + ks * 16);
+      qreg[ks] = qok ? v : u32x4_t{0u, 0u, 0u, 0u};
+    }
+  }
+  // keys [rlo, rhi) visible to the row; the block's smallest and largest bounds
+  const int rlo = qok ? min(row_first(a, r.row0 + qrel, qpos), klen) : 0;
+  const int rhi = qok ? max(qpos + 1, r.prefix) : 0;
+  int lo_min = attend_first(r.c + q_lo, a.window), lo_max = a.window > 0 ? max(r.c + q_hi - a.window, 0) : 0;
+  if (a.first_key) {
+    // every wavefront of a row block sees other positions: through LDS
+    int mn = qok ? rlo : 0x7fffffff, mx = qok ? rlo : 0;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      mn = min(mn, __shfl_xor(mn, o, 64));
+      mx = max(mx, __shfl_xor(mx, o, 64));
+    }
+    if (tid < 2) red[tid] = tid ? 0 : 0x7fffffff;
+    __syncthreads();
+    if (lane == 0) {
+      atomicMin(&red[0], mn);
+      atomicMax(&red[1], mx);
+    }
+    __syncthreads();
+    lo_min = __builtin_amdgcn_readfirstlane(red[0]);
+    lo_max = __builtin_amdgcn_readfirstlane(red[1]);
+  }
+  const int hi_min = max(r.c + q_lo + 1, r.prefix), hi_max = max(r.c + q_hi, r.prefix);
+  // this split's tiles: an even share of those that the window leaves, cut to
+  // those that hold a visible key
+  const int all0 = attend_first(r.c + q_lo, a.window) / KT, all1 = (hi_max + KT - 1) / KT;
+  const int share = (all1 - all0 + r.nsplit - 1) / r.nsplit;
+  const int t0 = max(all0 + sp * share, lo_min / KT), t1 = min(all0 + (sp + 1) * share, all1);
+
+  f32x16_t oacc[NOB];
+#pragma unroll
+  for (int ob = 0; ob < NOB; ++ob)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[ob][i] = 0.f;
+  float mrun = kNoScore, lrun = 0.f;
+  float slope = 0.f;
+  if constexpr (BIAS) slope = a.slopes[kh * G + hrow] * kLog2e;
+
+  const int32_t *bt = a.kv.bt + (size_t)r.seq * a.kv.max_pages;
+  const int npages = (klen + kPageSize - 1) / kPageSize;
+  constexpr int PPT = KT / kPageSize;
+  static_assert(PPT == 4, "tile = 4 pages");
+  typedef const __attribute__((address_space(4))) int32_t *bt_ptr_t;
+  const bt_ptr_t btc = (bt_ptr_t)bt;
+  auto bt_tile = [&](int t) -> i32x4_t {  // pages past the sequence repeat its last id (empty ranges below)
+    i32x4_t v;
+#pragma unroll
+    for (int j = 0; j < PPT; ++j) v[j] = btc[min(t * PPT + j, npages - 1)];
+    return v;
+  };
+  constexpr int ES = F8 ? 1 : 2;
+  constexpr uint32_t kHeadBytes = kPageSize * HD * ES;  // one page's block of a kv head
+  const uint64_t page_bytes = (uint64_t)a.nkv * kHeadBytes;
+  const uint8_t *const kbase = reinterpret_cast<const uint8_t *>(a.kv.k) + (size_t)kh * kHeadBytes;
+  const uint8_t *const vbase = reinterpret_cast<const uint8_t *>(a.kv.v) + (size_t)kh * kHeadBytes;
+  // page j of a tile as a buffer range over its keys below klen (empty for an
+  // id outside the pool): loads past it give zeros, without traffic
+  auto page_rsrc = [&](const uint8_t *base, const i32x4_t &btv, int j, int first_key) -> buf_rsrc_t {
+    const int phys = j == 0 ? btv[0] : j == 1 ? btv[1] : j == 2 ? btv[2] : btv[3];
+    const int rem = klen - first_key;
+    const bool live = (unsigned)phys < (unsigned)a.kv.num_pages && rem > 0;
+    const int range = __builtin_amdgcn_readfirstlane(live ? min(rem, kPageSize) * (HD * ES) : 0);
+    return make_rsrc(base + (uint64_t)(uint32_t)(live ? phys : 0) * page_bytes, range);
+  };
+  // --- bf16: load instruction i of wave w fills keys KPI (i 4 + w) .. + KPI - 1
+  // of a tile; lane l writes chunk position l % CPR of key .. + l / CPR.
+  // K chunk c of key t lies at c ^ (t & 7), V chunk c at c ^ 2 (t & 3).
+  constexpr int KPI = 1024 / ROW, NI = KT / (KPI * kWaves);
+  uint32_t koff[NI], voff[NI];
+  if constexpr (!F8) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int key = KPI * (i * kWaves + wave) + lane / CPR, pos = lane % CPR;
+      koff[i] = (uint32_t)((key % kPageSize) * ROW + 16 * (pos ^ (key & 7)));
+      voff[i] = (uint32_t)((key % kPageSize) * ROW + 16 * (pos ^ (2 * (key & 3))));
+    }
+  }
+  auto dma = [&](int t, const i32x4_t &btv, uint8_t *dst, bool is_v) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int key0 = KPI * (i * kWaves + wave), j = key0 / kPageSize;
+      lds_dma16(page_rsrc(is_v ? vbase : kbase, btv, j, t * KT + j * kPageSize), dst + key0 * ROW,
+                is_v ? voff[i] : koff[i]);
+    }
+  };
+  // --- 8 bits: unit u = tid + 256 i is 16 codes of key u / (HD / 16); they become two chunks
+  constexpr int CU = HD / 16, NF = KT * CU / 256;
+  u32x4_t kreg[F8 ? NF : 1], vreg[F8 ? NF : 1];
+  auto fetch = [&](int t, const i32x4_t &btv, u32x4_t (&reg)[F8 ? NF : 1], bool is_v) {
+#pragma unroll
+    for (int i = 0; i < (F8 ? NF : 0); ++i) {
+      const int key = (tid + 256 * i) / CU;
+      const int j = __builtin_amdgcn_readfirstlane(key / kPageSize);  // 64 / CU keys of one page per wavefront
+      reg[i] = buf_ld_u32x4<0>(page_rsrc(is_v ? vbase : kbase, btv, j, t * KT + j * kPageSize),
+                               (key % kPageSize) * HD + (tid % CU) * 16);
+    }
+  };
+  auto land = [&](const u32x4_t (&reg)[F8 ? NF : 1], uint8_t *dst, bool is_v) {
+#pragma unroll
+    for (int i = 0; i < (F8 ? NF : 0); ++i) {
+      const int key = (tid + 256 * i) / CU, ch = 2 * (tid % CU);
+      const int x = is_v ? 2 * (key & 3) : key & 7;
+      st_u32x4(dst + key * ROW + 16 * (ch ^ x), e4m3x8_to_bf16x8(u32x2_t{reg[i][0], reg[i][1]}));
+      st_u32x4(dst + key * ROW + 16 * ((ch + 1) ^ x), e4m3x8_to_bf16x8(u32x2_t{reg[i][2], reg[i][3]}));
+    }
+  };
+
+  // K operand of the scores: key kb 32 + lq, chunk 2 ks + lh
+  int kaddr[4];
+#pragma unroll
+  for (int k4 = 0; k4 < 4; ++k4) kaddr[k4] = lq * ROW + 16 * ((2 * k4 + lh) ^ (lq & 7));
+  // V^T operand, the transposing read: lane 16 g + 4 e + q points at key
+  // kb 32 + 16 jj + 8 h + 4 (g / 2) + e, dims ob 32 + 16 (g & 1) + 4 q .. + 3
+  const int tg = lane >> 4, te = (lane >> 2) & 3, tq = lane & 3;
+  int vaddr[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+    vaddr[b] = (4 * (tg >> 1) + te) * ROW + 16 * ((4 * b + 2 * (tg & 1) + (tq >> 1)) ^ (2 * te)) + 8 * (tq & 1);
+  typedef short v4s_t __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4s_t lds_v4s_t;
+  auto vt_read = [&](const uint8_t *vt, int ob, int kb, int jj, int h) -> u32x2_t {
+    const uint8_t *p = vt + vaddr[ob & 1] + (kb * 32 + 16 * jj + 8 * h) * ROW + 128 * (ob >> 1);
+    return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t *)p));
+  };
+  // S^T of the K tile at kt: lane value i of block kb at key 32 kb + 8 (i / 4) + 4 lh + i % 4
+  auto scores = [&](const uint8_t *kt, f32x16_t (&s)[2]) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const u32x4_t v = *reinterpret_cast<const u32x4_t *>(kt + kaddr[ks & 3] + 128 * (ks >> 2) + kb * 32 * ROW);
+        s[kb] = mfma32x32x16(v, qreg[ks], s[kb]);
+      }
+  };
+  // Values of a tile that some row does not see: a value that is not finite
+  // would reach those rows too, as 0 x inf.  Such values are set to zero in
+  // LDS, and the rows that do see them take them from the cache one by one.
+  // True if any was found; which of the two flags it uses follows the tile.
+  auto clean = [&](uint8_t *vt, int which) -> bool {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < TILE / 16 / 256; ++i) {
+      u32x4_t *p = reinterpret_cast<u32x4_t *>(vt + (i * 256 + tid) * 16);
+      u32x4_t v = *p;
+      bool here = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool b0 = (v[e] & 0x7F80u) == 0x7F80u, b1 = (v[e] & 0x7F800000u) == 0x7F800000u;
+        here |= b0 | b1;
+        v[e] &= (b0 ? 0xFFFF0000u : 0xFFFFFFFFu) & (b1 ? 0xFFFFu : 0xFFFFFFFFu);
+      }
+      if (here) *p = v;
+      bad |= here;
+    }
+    if (bad) odd[which] = 1;
+    if (tid == 0) odd[which ^ 1] = 0;  // read last before the barrier that ended the tile before
+    __syncthreads();
+    return odd[which] != 0;
+  };
+
+  if (t0 < t1) {
+    if (tid < 2) odd[tid] = 0;
+    f32x16_t sc[2];
+    i32x4_t bt1 = bt_tile(t0 + 1), bt2 = bt_tile(t0 + 2);
+    {
+      const i32x4_t b0 = bt_tile(t0);
+      if constexpr (F8) {
+        u32x4_t k1[NF];
+        fetch(t0, b0, kreg, false);
+        fetch(t0, b0, vreg, true);
+        fetch(t0 + 1, bt1, k1, false);
+        land(kreg, buf0, false);
+        land(vreg, buf0 + TILE, true);
+        land(k1, buf1, false);
+      } else {
+        dma(t0, b0, buf0, false);
+        dma(t0, b0, buf0 + TILE, true);
+        if (t0 + 1 < t1) dma(t0 + 1, bt1, buf1, false);
+      }
+    }
+    wait_loads<0>();
+    __syncthreads();
+    scores(buf0, sc);
+    __syncthreads();  // every wave past the scores of the first tile before K of the third refills its buffer
+    auto step = [&](int t, auto lastconst) {
+      constexpr bool LAST = decltype(lastconst)::value;
+      uint8_t *const cur = ((t - t0) & 1) ? buf1 : buf0, *const nxt = ((t - t0) & 1) ? buf0 : buf1;
+      const int k0 = t * KT;
+      f32x16_t scn[2];
+      // (before the next loads are issued: its barrier would wait for them)
+      const bool masked = k0 < lo_max || k0 + KT > hi_min;  // uniform over the block
+      const bool odd_values = masked && clean(cur + TILE, t & 1);
+      if constexpr (!LAST) {
+        // K of tile t and V of tile t - 1 were read before the last barrier
+        if constexpr (F8) {
+          fetch(t + 2, bt2, kreg, false);
+          fetch(t + 1, bt1, vreg, true);
+        } else {
+          if (t + 2 < t1) dma(t + 2, bt2, cur, false);
+          dma(t + 1, bt1, nxt + TILE, true);
+        }
+        bt1 = bt2;
+        bt2 = bt_tile(t + 3);
+      }
+      if constexpr (!LAST) scores(nxt, scn);
+      if constexpr (CAP || BIAS) {
+        const float d0 = (float)(qpos - k0 - 4 * lh);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float s = mod_score<CAP>(sc[kb][i], a.qscale, a.cap2);
+            if constexpr (BIAS) s = fmaf(-slope, fabsf(d0 - (float)(kb * 32 + 8 * (i >> 2) + (i & 3))), s);
+            sc[kb][i] = s;
+          }
+      }
+      if (masked) {
+        const int d = k0 + 4 * lh - rlo;
+        const unsigned span = (unsigned)max(rhi - rlo, 0);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            sc[kb][i] = (unsigned)(d + kb * 32 + 8 * (i >> 2) + (i & 3)) < span ? sc[kb][i] : kNoScore;
+      }
+      float mraw = kNoScore;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mraw = fmaxf(mraw, sc[kb][i]);
+      {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mraw), __float_as_uint(mraw), false, false);
+        mraw = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      }
+      constexpr bool RAW = !(CAP || BIAS);  // scores still to be scaled (qscale > 0 keeps their order)
+      const float ms = RAW ? mraw * a.qscale : mraw;
+      const bool bump = ms > mrun + kSlack;
+      const float mx = bump ? ms : mrun;
+      const float alpha = bump ? fast_exp2(mrun - mx) : 1.0f;
+      const float neg = mx != kNoScore ? -mx : 0.f;
+      float l = lrun * alpha;
+      uint32_t pk[2][8];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int pr = 0; pr < 8; ++pr) {
+          const float p0 = fast_exp2(RAW ? fmaf(sc[kb][2 * pr], a.qscale, neg) : sc[kb][2 * pr] + neg);
+          const float p1 = fast_exp2(RAW ? fmaf(sc[kb][2 * pr + 1], a.qscale, neg) : sc[kb][2 * pr + 1] + neg);
+          // P enters its product rounded to bf16 (half a step, 2^-9 of a
+          // probability); the sum keeps the fp32 values
+          pk[kb][pr] = pack_bf16x2(p0, p1);
+          l += p0 + p1;
+        }
+      // (the test on l, true for every finite sum, keeps this branch behind
+      // the block above, whose exponentials run under the score products)
+      const bool rescale = __builtin_amdgcn_ballot_w64(bump && mrun != kNoScore && l >= 0.f) != 0;
+      lrun = l;
+      mrun = mx;
+      if (__builtin_expect(rescale, 0)) {
+#pragma unroll
+        for (int ob = 0; ob < NOB; ++ob) oacc[ob] = oacc[ob] * alpha;
+      }
+      // O^T += V^T P^T: k-step j takes keys 16 (j % 2) + {0..3, 8..11} + 4 lh of key block j / 2
+      const uint8_t *const vt = cur + TILE;
+#pragma unroll
+      for (int ob = 0; ob < NOB; ++ob) {
+        f32x16_t acc = oacc[ob];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int kb = j >> 1, jj = j & 1;
+          const u32x2_t v0 = vt_read(vt, ob, kb, jj, 0), v1 = vt_read(vt, ob, kb, jj, 1);
+          const u32x4_t av = {v0[0], v0[1], v1[0], v1[1]};
+          const u32x4_t bv = {pk[kb][4 * jj], pk[kb][4 * jj + 1], pk[kb][4 * jj + 2], pk[kb][4 * jj + 3]};
+          acc = mfma32x32x16(av, bv, acc);
+        }
+        oacc[ob] = acc;
+      }
+      if (__builtin_expect(odd_values, 0)) {
+        // the values that were set to zero, for the rows that see their keys:
+        // a sum with one of them is what that value makes of it
+        for (int key = max(k0, rlo); key < min(k0 + KT, rhi); ++key) {
+          const int phys = bt[key / kPageSize];
+          if ((unsigned)phys >= (unsigned)a.kv.num_pages) continue;
+          const size_t e0 = ((size_t)phys * a.nkv + kh) * (kPageSize * HD) + (size_t)(key % kPageSize) * HD;
+#pragma unroll
+          for (int ob = 0; ob < NOB; ++ob)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const size_t e = e0 + ob * 32 + 8 * (i >> 2) + 4 * lh + (i & 3);
+              uint32_t w;
+              if constexpr (F8)
+                w = e4m3x2_to_bf16x2<false>(a.kv.v8()[e]) & 0xFFFFu;
+              else
+                w = a.kv.v[e];
+              if ((w & 0x7F80u) == 0x7F80u) oacc[ob][i] += bf16_lo(w);
+            }
+        }
+      }
+      if constexpr (!LAST) {
+        if constexpr (F8) {
+          land(kreg, cur, false);
+          land(vreg, nxt + TILE, true);
+        }
+        sc[0] = scn[0];
+        sc[1] = scn[1];
+        wait_loads<0>();
+        __syncthreads();
+      }
+    };
+    for (int t = t0; t + 1 < t1; ++t) step(t, std::false_type{});
+    step(t1 - 1, std::true_type{});
+  }
+  float l = lrun;
+  l += shfl_xor_f32(l, 32);
+  if (!qok) return;
+  const float vscale = F8 ? a.kv.vs : 1.f;
+  const int qh = kh * G + hrow;
+  if (r.nsplit == 1) {
+    const bool empty = rlo >= rhi;
+    const float inv = empty ? 0.f : vscale / l;
+    const size_t at = (size_t)(r.row0 + qrel) * a.nq + qh;
+    uint16_t *dst = a.out + at * HD + 4 * lh;
+#pragma unroll
+    for (int ob = 0; ob < NOB; ++ob)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const u32x2_t w = {pack_bf16x2(oacc[ob][4 * g] * inv, oacc[ob][4 * g + 1] * inv),
+                           pack_bf16x2(oacc[ob][4 * g + 2] * inv, oacc[ob][4 * g + 3] * inv)};
+        *reinterpret_cast<u32x2_t *>(dst + ob * 32 + 8 * g) = w;
+      }
+    if (lh == 0 && a.lse) a.lse[at] = empty ? kNoScore : kLn2 * (mrun + log2f(l));
+    return;
+  }
+  const size_t slot = ((size_t)m[PRE_PART0 * a.n + r.k] + (size_t)qrel * r.nsplit + sp) * a.nq + qh;
+  float *dst = a.part_o + slot * HD + 4 * lh;
+#pragma unroll
+  for (int ob = 0; ob < NOB; ++ob)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<f32x4_t *>(dst + ob * 32 + 8 * g) =
+          f32x4_t{oacc[ob][4 * g] * vscale, oacc[ob][4 * g + 1] * vscale, oacc[ob][4 * g + 2] * vscale,
+                  oacc[ob][4 * g + 3] * vscale};
+  if (lh == 0) {
+    a.part_ml[slot * 2] = mrun;
+    a.part_ml[slot * 2 + 1] = l;
+  }
+}
+
+// Joins the splits of the rows that have several, one wavefront per (row, head).
+template <int HD>
+__global__ __launch_bounds__(256) void k_attend_chunk_combine(AttendArgs a) {
+  const int32_t *m = meta_words(a);
+  const int lane = threadIdx.x & 63;
+  // (requests without splits share the next one's first row: the last entry
+  // at or below the row is a request that has splits, or the row's own)
+  const PreReq r = pre_req(a, m, last_at_or_below(m + PRE_COMB0 * a.n, a.n, blockIdx.x));
+  const int qh = blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (qh >= a.nq) return;
+  const int j = blockIdx.x - m[PRE_COMB0 * a.n + r.k], p = r.c + j;
+  const bool empty = row_first(a, r.row0 + j, p) >= max(p + 1, r.prefix);
+  const size_t base = ((size_t)m[PRE_PART0 * a.n + r.k] + (size_t)j * r.nsplit) * a.nq + qh;
+  join_splits<HD>(a, base, r.nsplit, (size_t)(r.row0 + j) * a.nq + qh, empty, lane);
+}
+
+}  // namespace
+
+hipError_t launch_attend_chunk(const Shape &s, const AttendCall &c, const AttendArgs &a, hipStream_t st) {
+  const AttendPlan &p = *c.plan;
+  const dim3 grid(p.pre_tiles * s.nkv);
+#define EB_CHUNK(HD_, F8_)                                                                                     \
+  do {                                                                                                         \
+    if (c.softcap > 0.f && c.slopes)                                                                           \
+      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, true, true>), grid, dim3(256), 0, st, a);                   \
+    else if (c.softcap > 0.f)                                                                                  \
+      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, true, false>), grid, dim3(256), 0, st, a);                  \
+    else if (c.slopes)                                                                                         \
+      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, false, true>), grid, dim3(256), 0, st, a);                  \
+    else                                                                                                       \
+      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, false, false>), grid, dim3(256), 0, st, a);                 \
+  } while (0)
+  if (s.hd == 128) {
+    if (a.kv.f8)
+      EB_CHUNK(128, true);
+    else
+      EB_CHUNK(128, false);
+  } else {
+    if (a.kv.f8)
+      EB_CHUNK(64, true);
+    else
+      EB_CHUNK(64, false);
+  }
+#undef EB_CHUNK
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (p.pre_comb_rows > 0) {
+    const dim3 cg(p.pre_comb_rows, (s.nq + 3) / 4);
+    if (s.hd == 128)
+      hipLaunchKernelGGL(k_attend_chunk_combine<128>, cg, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL(k_attend_chunk_combine<64>, cg, dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace eb

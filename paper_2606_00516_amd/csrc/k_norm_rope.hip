@@ -96,16 +96,6 @@ hipError_t launch_rmsnorm(const uint16_t *x, const uint16_t *gamma, uint16_t *ou
 // RoPE (rotate-half pairs (t, t + hd/2), frequency theta^(-2t/hd), angle
 // formed in fp64) on the q and k heads of one QKV row, q rotated in place,
 // rotated k and v stored at the row's slot of its request's paged cache.
-// Codes of eight bf16 values (packed pairs) divided by scale.
-__device__ __forceinline__ u32x2_t e4m3x8_of_bf16x8(u32x4_t w, float scale) {
-  u32x2_t r;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    r[i] = e4m3x4_from_f32(bf16_lo(w[2 * i]) / scale, bf16_hi(w[2 * i]) / scale, bf16_lo(w[2 * i + 1]) / scale,
-                           bf16_hi(w[2 * i + 1]) / scale);
-  return r;
-}
-
 // One block per row; a thread moves 8 consecutive dims of one half of a
 // head and their 8 partners in 16-byte accesses.  The angle pos * freq is
 // formed and reduced to [-pi, pi] in fp64; its sine and cosine are then

@@ -1,0 +1,110 @@
+#include <hip/hip_runtime.h>
+
+#include "op_plan.h"
+
+#include <algorithm>
+#include <numeric>
+
+namespace eb {
+
+namespace {
+// Splits of the keys of a chunk: enough blocks to fill the chip if this were
+// its only request, each long enough that the partials (fp32 rows written and
+// read again) stay small beside the keys it reads.
+int32_t chunk_splits(int32_t rows, int32_t kv_heads, int32_t q_blocks, int32_t tiles) {
+  const int32_t items = q_blocks * kv_heads;
+  const int32_t least = rows <= kAttendRows ? 8 : 16;  // tiles per split
+  return std::max(1, std::min((512 + items - 1) / items, tiles / least));
+}
+}  // namespace
+
+void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
+                 int32_t weight_rows, AttendPlan &p) {
+  p = AttendPlan();
+  p.T = b.num_tokens;
+  const int32_t G = cfg.n_q_heads / cfg.n_kv_heads, nkv = cfg.n_kv_heads, bq = kAttendRows / G;
+  std::vector<int32_t> ones, many, row(b.num_seqs + 1, 0);
+  for (int i = 0; i < b.num_seqs; ++i) {
+    row[i + 1] = row[i] + b.chunk_lens_host[i];
+    (b.chunk_lens_host[i] == 1 ? ones : many).push_back(i);
+  }
+  const auto keys_of = [&](int i) { return b.context_lens_host[i] + b.chunk_lens_host[i]; };
+  p.n_dec = (int32_t)ones.size();
+  p.dec.assign((size_t)DEC_FIELDS * p.n_dec + 1, 0);
+  int64_t runs = 0;
+  for (int32_t d = 0; d < p.n_dec; ++d) {
+    const int i = ones[d];
+    const int32_t c = b.context_lens_host[i], keys = c + 1 - attend_first(c, window);
+    const int32_t per = attend_split_keys(keys), ns = (keys + per - 1) / per;
+    int32_t *f = p.dec.data() + d;
+    const size_t n = (size_t)p.n_dec;
+    f[DEC_SEQ * n] = i;
+    f[DEC_ROW * n] = row[i];
+    f[DEC_CTX * n] = c;
+    f[DEC_SPLIT0 * n] = p.dec_splits;
+    f[DEC_WBLOCK0 * n] = p.dec_wblocks;
+    f[DEC_SCORE0 * n] = (int32_t)runs;
+    p.dec_splits += ns;
+    if (ns > 1) p.dec_combine = true;
+    if (weights) {
+      p.dec_wblocks += (keys + kWeightSpan - 1) / kWeightSpan;
+      runs += (int64_t)((keys + 15) / 16) * cfg.n_q_heads;
+    }
+  }
+  std::stable_sort(many.begin(), many.end(), [&](int32_t x, int32_t y) { return keys_of(x) > keys_of(y); });
+  p.n_pre = (int32_t)many.size();
+  p.pre.assign((size_t)PRE_FIELDS * p.n_pre + 1, 0);
+  int32_t part = p.dec_splits;
+  for (int32_t k = 0; k < p.n_pre; ++k) {
+    const int i = many[k];
+    const int32_t c = b.context_lens_host[i], n = b.chunk_lens_host[i], nqb = (n + bq - 1) / bq;
+    // the most tiles of any block of rows: the last one's, or with a prefix
+    // past it the first one's behind the window
+    int32_t tiles = 0;
+    for (int32_t q = 0; q < nqb; q = q + 1 < nqb ? nqb - 1 : nqb) {
+      const int32_t first = attend_first(c + q * bq, window) / kAttendTile;
+      const int32_t end = std::max(c + std::min(n, (q + 1) * bq), prefix ? prefix[i] : 0);
+      tiles = std::max(tiles, (end + kAttendTile - 1) / kAttendTile - first);
+    }
+    const int32_t ns = chunk_splits(n * G, nkv, nqb, tiles);
+    const size_t m = (size_t)p.n_pre;
+    int32_t *f = p.pre.data() + k;
+    f[PRE_SEQ * m] = i;
+    f[PRE_ROW * m] = row[i];
+    f[PRE_CTX * m] = c;
+    f[PRE_LEN * m] = n;
+    f[PRE_PREFIX * m] = prefix ? prefix[i] : 0;
+    f[PRE_TILE0 * m] = p.pre_tiles;
+    f[PRE_NSPLIT * m] = ns;
+    f[PRE_PART0 * m] = part;
+    f[PRE_COMB0 * m] = p.pre_comb_rows;
+    f[PRE_WBLOCK0 * m] = p.pre_wblocks;
+    p.pre_tiles += nqb * ns;
+    if (ns > 1) {
+      part += n * ns;
+      p.pre_comb_rows += n;
+    }
+    if (weights) {
+      // every new key gets its first value, every key that a counted row may
+      // see gets its share
+      const int32_t j0 = weight_rows > 0 ? std::max(0, n - weight_rows) : 0;
+      const int32_t first = std::min(c, attend_first(c + j0, window)) / kWeightKeys;
+      p.pre_wblocks += (c + n + kWeightKeys - 1) / kWeightKeys - first;
+    }
+  }
+  size_t off = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off = (off + bytes + 255) / 256 * 256;
+    return o;
+  };
+  p.o_dec = take(p.dec.size() * 4);
+  p.o_pre = take(p.pre.size() * 4);
+  p.o_lse = weights ? take((size_t)p.T * cfg.n_q_heads * 4) : 0;
+  p.o_part_o = take((size_t)part * cfg.n_q_heads * cfg.head_dim * 4);
+  p.o_part_ml = take((size_t)part * cfg.n_q_heads * 8);
+  p.o_scores = take((size_t)runs * 64);
+  p.total = off;
+}
+
+}  // namespace eb

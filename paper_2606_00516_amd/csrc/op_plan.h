@@ -1,0 +1,58 @@
+// Host planning of the cache operators: pure C++, no HIP calls.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include <vector>
+
+#include "../../include/eb_layer.h"
+
+namespace eb {
+
+constexpr int kAttendTile = 64;    // keys per step of a chunk's rows
+constexpr int kAttendRows = 128;   // query rows (positions x heads of the group) per block
+constexpr int kWeightKeys = 128;   // keys per block of the weights pass of a chunk
+constexpr int kWeightSpan = 1024;  // keys per block of the weights pass of a decode row
+
+// Keys per split of a decode row that sees `keys` of them, a multiple of the
+// page.  It follows from the request alone, so that its result does not
+// depend on the batch.
+__host__ __device__ inline int32_t attend_split_keys(int32_t keys) {
+  return keys <= 1024 ? 128 : keys <= 4096 ? 256 : 512;
+}
+// First key (of a whole page) that the row at position p may see.
+__host__ __device__ inline int32_t attend_first(int32_t p, int32_t window) {
+  return window > 0 && p >= window ? (p - window + 1) & ~15 : 0;
+}
+
+// Tables of one attention call.  Decode part: requests with one new row, in
+// batch order; chunk part: the others, the most keys first.  Each table is a
+// run of arrays (below) of n entries, then one closing word.
+struct AttendPlan {
+  int32_t T = 0;
+  int32_t n_dec = 0, dec_splits = 0, dec_wblocks = 0;
+  bool dec_combine = false;
+  std::vector<int32_t> dec;
+  int32_t n_pre = 0, pre_tiles = 0, pre_comb_rows = 0, pre_wblocks = 0;
+  std::vector<int32_t> pre;
+  // byte offsets in the workspace (256-byte aligned)
+  size_t o_dec = 0, o_pre = 0, o_lse = 0, o_part_o = 0, o_part_ml = 0, o_scores = 0, total = 0;
+};
+
+// request, row, context, first split, first block of the weights pass, first
+// 16-score run
+enum DecField { DEC_SEQ = 0, DEC_ROW, DEC_CTX, DEC_SPLIT0, DEC_WBLOCK0, DEC_SCORE0, DEC_FIELDS };
+// request, first row, context, rows, prefix, first tile, splits of the keys,
+// first partial, first row among those with several splits, first block of
+// the weights pass
+enum PreField {
+  PRE_SEQ = 0, PRE_ROW, PRE_CTX, PRE_LEN, PRE_PREFIX, PRE_TILE0, PRE_NSPLIT, PRE_PART0, PRE_COMB0, PRE_WBLOCK0,
+  PRE_FIELDS
+};
+
+// window 0: none; prefix: per request, or null.  The batch has passed
+// check_batch.
+void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
+                 int32_t weight_rows, AttendPlan &p);
+
+}  // namespace eb
