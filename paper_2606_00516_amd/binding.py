@@ -225,7 +225,10 @@ class Handle:
 
     def __init__(self, shape, max_seqs: int, max_tokens: int):
         self.shape = shape
-        self.cfg = config_of(shape)
+        self.cfg = c = config_of(shape)
+        self.n_q_heads, self.n_kv_heads, self.head_dim = c.n_q_heads, c.n_kv_heads, c.head_dim
+        self.qkv_cols = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim
+        self.page_keys = c.n_kv_heads * c.page_size   # keys of one page over the kv heads
         h = ctypes.c_void_p()
         _check(lib().eb_create(ctypes.byref(self.cfg), int(max_seqs), int(max_tokens), ctypes.byref(h)))
         self.h = h
@@ -520,17 +523,22 @@ def eb_op_gather_kv(h: Handle, k_cache, v_cache, block_tables, context_lens, chu
 # caller's to keep.
 # ---------------------------------------------------------------------------
 
-def _dev(t: torch.Tensor, dtype, name: str, numel: Optional[int] = None):
-    """Device address of a contiguous GPU tensor of this dtype (and size)."""
-    if t.dtype != dtype:
+def _dev(t: torch.Tensor, dtype, name: str, numel: int = -1, dev: int = -1):
+    """Device address of a contiguous GPU tensor of this dtype (and size), on
+    device dev (-1: the current one)."""
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.get_device() != (dev if dev >= 0 else torch.cuda.current_device()):   # (a CPU tensor's is -1)
         raise ValueError(f"{name} must be on the current GPU")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if numel is not None and t.numel() != numel:
+    if numel >= 0 and t.numel() != numel:
         raise ValueError(f"{name} must have {numel} elements")
     return t.data_ptr()
+
+
+def _raw_stream(stream, dev: int):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _lens(a, name: str) -> np.ndarray:
@@ -542,13 +550,17 @@ def _lens(a, name: str) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
-def _ws(ws: Optional[torch.Tensor], nbytes, stream):
+def _addr(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]
+
+
+def _ws(ws: Optional[torch.Tensor], nbytes, stream, dev: int):
     """(tensor to keep alive, address, bytes) of a workspace; allocated when None."""
     if ws is None:
         ws = alloc_workspace(nbytes())
         if stream is not None:  # its memory is not given out again before that stream is done with it
             ws.record_stream(stream)
-    return ws, _dev(ws, torch.uint8, "ws"), ws.numel()
+    return ws, _dev(ws, torch.uint8, "ws", -1, dev), ws.numel()
 
 
 def rotary(theta: float, rotary_dim: int = 0, layout: str = "half", scaling: str = "none", factor: float = 1.0,
@@ -572,12 +584,11 @@ def eb_op_rotary_kv_append(h: Handle, rot: Rotary, qkv: torch.Tensor, kv: Option
                            positions: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
     """Rotates the q heads of qkv in place and stores rotated k and v in the
     cache (kv None: rotates k in place too); returns qkv."""
-    T, s = batch.c.num_tokens, h.cfg
-    p = _dev(qkv, torch.bfloat16, "qkv", T * (s.n_q_heads + 2 * s.n_kv_heads) * s.head_dim)
-    pos = None if positions is None else _dev(positions, torch.int32, "positions", T)
-    held, wp, wn = _ws(ws, lambda: eb_op_rotary_kv_append_workspace_bytes(h, batch), stream)
-    _check(lib().eb_op_rotary_kv_append(h.h, ctypes.byref(rot), p, None if kv is None else ctypes.byref(kv),
-                                        ctypes.byref(batch.c), pos, wp, wn, _stream(stream)))
+    T, dev = batch.c.num_tokens, torch.cuda.current_device()
+    p = _dev(qkv, torch.bfloat16, "qkv", T * h.qkv_cols, dev)
+    pos = None if positions is None else _dev(positions, torch.int32, "positions", T, dev)
+    held, wp, wn = _ws(ws, lambda: eb_op_rotary_kv_append_workspace_bytes(h, batch), stream, dev)
+    _check(_lib.eb_op_rotary_kv_append(h.h, rot, p, kv, batch.c, pos, wp, wn, _raw_stream(stream, dev)))
     return qkv
 
 
@@ -593,14 +604,16 @@ def score_mod(scale: float = 0.0, softcap: float = 0.0, slopes: Optional[torch.T
 
 
 def _check_mod(h: Handle, batch: HostBatch, m: Optional[ScoreMod]):
-    slopes, first, pre = m.held if m is not None else (None, None, None)
-    if slopes is not None and slopes.numel() != h.cfg.n_q_heads:
+    if m is None:
+        return None
+    slopes, first, pre = m.held
+    if slopes is not None and slopes.numel() != h.n_q_heads:
         raise ValueError("slopes needs one value per query head")
     if first is not None and first.numel() != batch.c.num_tokens:
         raise ValueError("first_key needs one value per row")
     if pre is not None and len(pre) != batch.c.num_seqs:
         raise ValueError("prefix_lens needs one value per request")
-    return None if m is None else ctypes.byref(m)
+    return m
 
 
 def eb_op_attention_mod_workspace_bytes(h: Handle, batch: HostBatch, mod: Optional[ScoreMod] = None,
@@ -615,20 +628,18 @@ def eb_op_attention_mod(h: Handle, qkv: torch.Tensor, kv: KvCache, batch: HostBa
                         ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention with modified scores and masks; out bf16 [T, n_q head_dim],
     lse fp32 [T, n_q] and kv_weights fp32 [pages, n_kv, 16] where wanted."""
-    T, s = batch.c.num_tokens, h.cfg
-    p = _dev(qkv, torch.bfloat16, "qkv", T * (s.n_q_heads + 2 * s.n_kv_heads) * s.head_dim)
+    T, nq, dev = batch.c.num_tokens, h.n_q_heads, torch.cuda.current_device()
+    p = _dev(qkv, torch.bfloat16, "qkv", T * h.qkv_cols, dev)
     if out is None:
-        out = torch.empty(T, s.n_q_heads * s.head_dim, dtype=torch.bfloat16, device=qkv.device)
+        out = torch.empty(T, nq * h.head_dim, dtype=torch.bfloat16, device=qkv.device)
         if stream is not None:
             out.record_stream(stream)
-    o = _dev(out, torch.bfloat16, "out", T * s.n_q_heads * s.head_dim)
-    z = None if lse is None else _dev(lse, torch.float32, "lse", T * s.n_q_heads)
-    w = None if kv_weights is None else _dev(kv_weights, torch.float32, "kv_weights",
-                                             kv.num_pages * s.n_kv_heads * s.page_size)
+    o = _dev(out, torch.bfloat16, "out", T * nq * h.head_dim, dev)
+    z = None if lse is None else _dev(lse, torch.float32, "lse", T * nq, dev)
+    w = None if kv_weights is None else _dev(kv_weights, torch.float32, "kv_weights", kv.num_pages * h.page_keys, dev)
     m = _check_mod(h, batch, mod)
-    held, wp, wn = _ws(ws, lambda: eb_op_attention_mod_workspace_bytes(h, batch, mod, w is not None), stream)
-    _check(lib().eb_op_attention_mod(h.h, p, ctypes.byref(kv), ctypes.byref(batch.c), m, o, z, w, int(weight_rows),
-                                     wp, wn, _stream(stream)))
+    held, wp, wn = _ws(ws, lambda: eb_op_attention_mod_workspace_bytes(h, batch, mod, w is not None), stream, dev)
+    _check(_lib.eb_op_attention_mod(h.h, p, kv, batch.c, m, o, z, w, weight_rows, wp, wn, _raw_stream(stream, dev)))
     return out
 
 
@@ -647,18 +658,17 @@ def eb_op_kv_evict(h: Handle, src: KvCache, kv_weights: torch.Tensor, lens, keep
     a, b = _lens(lens, "lens"), _lens(keep_lens, "keep_lens")
     if len(a) != len(b):
         raise ValueError("lens and keep_lens need one value per request each")
-    s = h.cfg
-    w = _dev(kv_weights, torch.float32, "kv_weights", src.num_pages * s.n_kv_heads * s.page_size)
-    d = None if dst_weights is None else _dev(dst_weights, torch.float32, "dst_weights",
-                                              dst.num_pages * s.n_kv_heads * s.page_size)
+    dev = torch.cuda.current_device()
+    w = _dev(kv_weights, torch.float32, "kv_weights", src.num_pages * h.page_keys, dev)
+    d = None if dst_weights is None else _dev(dst_weights, torch.float32, "dst_weights", dst.num_pages * h.page_keys, dev)
     k, stride = None, 0
     if kept is not None:
-        if kept.dim() != 3 or kept.shape[0] != len(a) or kept.shape[1] != s.n_kv_heads:
+        if kept.dim() != 3 or kept.shape[0] != len(a) or kept.shape[1] != h.n_kv_heads:
             raise ValueError("kept must be [requests, n_kv, keys]")
-        k, stride = _dev(kept, torch.int32, "kept"), kept.shape[2]
-    held, wp, wn = _ws(ws, lambda: eb_op_kv_evict_workspace_bytes(h, a, b), stream)
-    _check(lib().eb_op_kv_evict(h.h, ctypes.byref(src), w, len(a), a.ctypes.data, b.ctypes.data, int(sink),
-                                int(recent), ctypes.byref(dst), d, k, int(stride), wp, wn, _stream(stream)))
+        k, stride = _dev(kept, torch.int32, "kept", -1, dev), kept.shape[2]
+    held, wp, wn = _ws(ws, lambda: eb_op_kv_evict_workspace_bytes(h, a, b), stream, dev)
+    _check(_lib.eb_op_kv_evict(h.h, src, w, len(a), _addr(a), _addr(b), sink, recent, dst, d, k, stride, wp, wn,
+                               _raw_stream(stream, dev)))
     return np.minimum(a, b)
 
 

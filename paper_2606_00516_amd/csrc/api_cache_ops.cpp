@@ -144,35 +144,16 @@ eb_status check_mod(const eb_score_mod *m, const eb_batch *b) {
 }
 
 // ---------------------------------------------------------------- eviction
-struct EvictPlan {
-  std::vector<int32_t> words;  // [S] lengths, [S] kept, [S + 1] first page group
-  long groups = 0;
-  int32_t max_len = 0, max_keep = 0;
-};
-constexpr int kGroupKeys = 64;  // keys per destination page group
-
-eb_status plan_evict(int32_t S, const int32_t *lens, const int32_t *keep, EvictPlan &p) {
+eb_status check_evict(int32_t n_kv, int32_t S, const int32_t *lens, const int32_t *keep, EvictPlan &p) {
   if (S < 0) return api_fail(EB_ERR_BATCH, "negative num_seqs");
   if (S > 0 && (!lens || !keep)) return api_fail(EB_ERR_NULL, "lens_host or keep_lens_host is NULL");
-  p.words.assign((size_t)3 * S + 1, 0);
   for (int i = 0; i < S; ++i) {
     if (lens[i] < 0 || keep[i] < 0)
       return api_fail(EB_ERR_BATCH, "request " + std::to_string(i) + ": negative length");
     if (lens[i] > 0x3FFFFFFF) return api_fail(EB_ERR_BATCH, "request " + std::to_string(i) + ": length overflows");
-    const int32_t k = std::min(lens[i], keep[i]);
-    p.words[i] = lens[i];
-    p.words[S + i] = keep[i];
-    p.words[(size_t)2 * S + i] = (int32_t)p.groups;
-    p.groups += (k + kGroupKeys - 1) / kGroupKeys;
-    p.max_len = std::max(p.max_len, lens[i]);
-    p.max_keep = std::max(p.max_keep, k);
-    if (p.groups > 0x3FFFFFFF) return api_fail(EB_ERR_LIMITS, "more kept keys than a launch holds");
   }
-  p.words[(size_t)3 * S] = (int32_t)p.groups;
+  if (!plan_evict(n_kv, S, lens, keep, p)) return api_fail(EB_ERR_LIMITS, "more keys than a launch holds");
   return EB_OK;
-}
-size_t evict_kept_bytes(const HandleView &v, int32_t S, const EvictPlan &p) {
-  return round_up((size_t)S * v.shape->nkv * p.max_keep * 4);
 }
 
 }  // namespace
@@ -307,8 +288,8 @@ size_t eb_op_kv_evict_workspace_bytes(const eb_handle *h, int32_t num_seqs, cons
                                       const int32_t *keep_lens_host) {
   return guarded_bytes([&]() -> size_t {
     EvictPlan p;
-    if (!h || plan_evict(num_seqs, lens_host, keep_lens_host, p) != EB_OK) return 0;
-    return round_up(p.words.size() * 4) + evict_kept_bytes(api_view(h), num_seqs, p);
+    if (!h || check_evict(api_view(h).shape->nkv, num_seqs, lens_host, keep_lens_host, p) != EB_OK) return 0;
+    return p.total;
   });
 }
 
@@ -326,7 +307,7 @@ eb_status eb_op_kv_evict(eb_handle *h, const eb_kv_cache *src, const float *kv_w
         (src->kv_dtype == EB_KV_FP8_E4M3 && (src->k_scale != dst->k_scale || src->v_scale != dst->v_scale)))
       return api_fail(EB_ERR_CONFIG, "source and destination must have the same element type and scales");
     EvictPlan p;
-    s = plan_evict(num_seqs, lens_host, keep_lens_host, p);
+    s = check_evict(v.shape->nkv, num_seqs, lens_host, keep_lens_host, p);
     if (s != EB_OK) return s;
     if (num_seqs > v.max_seqs) return api_fail(EB_ERR_LIMITS, "batch larger than the handle's max_seqs");
     if (sink < 0 || recent < 0) return api_fail(EB_ERR_CONFIG, "sink and recent must not be negative");
@@ -347,8 +328,7 @@ eb_status eb_op_kv_evict(eb_handle *h, const eb_kv_cache *src, const float *kv_w
     if (s != EB_OK) return s;
     if (kept && kept_stride < p.max_keep)
       return api_fail(EB_ERR_CONFIG, "kept_stride is smaller than the largest number of kept keys");
-    const size_t words = round_up(p.words.size() * 4);
-    s = api_check_ws(ws, ws_bytes, words + evict_kept_bytes(v, num_seqs, p));
+    s = api_check_ws(ws, ws_bytes, p.total);
     if (s == EB_OK) s = check_device(v);
     if (s != EB_OK) return s;
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -381,14 +361,12 @@ eb_status eb_op_kv_evict(eb_handle *h, const eb_kv_cache *src, const float *kv_w
     c.dst = api_kv(dst);
     c.weights = kv_weights;
     c.dst_weights = dst_weights;
-    c.kept = kept ? kept : reinterpret_cast<int32_t *>(static_cast<char *>(ws) + words);
+    c.ws = static_cast<char *>(ws);
+    c.kept = kept ? kept : reinterpret_cast<int32_t *>(c.ws + p.o_kept);
     c.kept_stride = kept ? kept_stride : p.max_keep;
-    c.S = num_seqs;
     c.sink = sink;
     c.recent = recent;
-    c.max_len = p.max_len;
-    c.groups = p.groups;
-    c.table = Table{p.words.data(), p.words.size(), static_cast<int32_t *>(ws)};
+    c.plan = &p;
     const hipError_t e = launch_evict(*v.shape, c, st);
     return e == hipSuccess ? EB_OK : api_hip_fail(e, "eviction");
   });

@@ -48,8 +48,16 @@ __device__ __forceinline__ PreReq pre_req(const AttendArgs &a, const int32_t *m,
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
-template <int HD, bool F8, bool CAP, bool BIAS>
+// How scores are made.  kCapped (no bias, a cap up to kCappedMost) needs no
+// running maximum: |s| <= 92 in log2 units keeps 2^s and sums of 2^30 of them
+// inside fp32 and bf16 alike.
+enum Mode { kPlain = 0, kCapped, kBiased, kCapBiased };
+constexpr float kCappedMost = 64.0f;
+
+template <int HD, bool F8, int MODE>
 __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
+  constexpr bool CAP = MODE == kCapped || MODE == kCapBiased, BIAS = MODE == kBiased || MODE == kCapBiased;
+  constexpr bool FIXED = MODE == kCapped;
   constexpr int KT = kAttendTile;
   constexpr int ROW = HD * 2;        // bytes per key row in LDS
   constexpr int CPR = ROW / 16;      // 16-byte chunks per row
@@ -124,9 +132,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
   for (int ob = 0; ob < NOB; ++ob)
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[ob][i] = 0.f;
-  float mrun = kNoScore, lrun = 0.f;
+  float mrun = FIXED ? 0.f : kNoScore, lrun = 0.f;
   float slope = 0.f;
-  if constexpr (BIAS) slope = a.slopes[kh * G + hrow] * kLog2e;
+  if constexpr (BIAS) slope = a.slopes ? a.slopes[kh * G + hrow] * kLog2e : 0.f;
 
   const int32_t *bt = a.kv.bt + (size_t)r.seq * a.kv.max_pages;
   const int npages = (klen + kPageSize - 1) / kPageSize;
@@ -298,19 +306,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
         bt1 = bt2;
         bt2 = bt_tile(t + 3);
       }
-      if constexpr (!LAST) scores(nxt, scn);
-      if constexpr (CAP || BIAS) {
-        const float d0 = (float)(qpos - k0 - 4 * lh);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float s = mod_score<CAP>(sc[kb][i], a.qscale, a.cap2);
-            if constexpr (BIAS) s = fmaf(-slope, fabsf(d0 - (float)(kb * 32 + 8 * (i >> 2) + (i & 3))), s);
-            sc[kb][i] = s;
-          }
-      }
-      if (masked) {
+      auto hide = [&]() {  // keys outside the row's range
+        asm volatile("");  // (a branch, not 32 selects in every tile)
         const int d = k0 + 4 * lh - rlo;
         const unsigned span = (unsigned)max(rhi - rlo, 0);
 #pragma unroll
@@ -318,30 +315,63 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             sc[kb][i] = (unsigned)(d + kb * 32 + 8 * (i >> 2) + (i & 3)) < span ? sc[kb][i] : kNoScore;
+      };
+      // plain scores are hidden before the next tile's are formed, so that
+      // nothing splits the run of products and exponentials below
+      if (MODE == kPlain && masked) hide();
+      if constexpr (!LAST) scores(nxt, scn);
+      if constexpr (CAP) {
+        if (all_small<2>(sc, a)) {
+          asm volatile("");  // (a branch: not both forms and a select)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[kb][i] = small_score(sc[kb][i], a);
+        } else {
+          asm volatile("");
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[kb][i] = mod_score<true>(sc[kb][i], a.qscale, a.cap2);
+        }
       }
-      float mraw = kNoScore;
+      if constexpr (BIAS) {
+        const float d0 = (float)(qpos - k0 - 4 * lh);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mraw = fmaxf(mraw, sc[kb][i]);
-      {
+          for (int i = 0; i < 16; ++i) {
+            const float s = CAP ? sc[kb][i] : sc[kb][i] * a.qscale;
+            sc[kb][i] = fmaf(-slope, fabsf(d0 - (float)(kb * 32 + 8 * (i >> 2) + (i & 3))), s);
+          }
+      }
+      if (MODE != kPlain && masked) hide();
+      constexpr bool RAW = MODE == kPlain;  // scores still to be scaled (qscale > 0 keeps their order)
+      float mx = 0.f, alpha = 1.f, neg = 0.f;
+      bool bump = false;
+      if constexpr (!FIXED) {
+        float mraw = kNoScore;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mraw = fmaxf(mraw, sc[kb][i]);
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mraw), __float_as_uint(mraw), false, false);
         mraw = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        const float ms = RAW ? mraw * a.qscale : mraw;
+        bump = ms > mrun + kSlack;
+        mx = bump ? ms : mrun;
+        alpha = bump ? fast_exp2(mrun - mx) : 1.0f;
+        neg = mx != kNoScore ? -mx : 0.f;
       }
-      constexpr bool RAW = !(CAP || BIAS);  // scores still to be scaled (qscale > 0 keeps their order)
-      const float ms = RAW ? mraw * a.qscale : mraw;
-      const bool bump = ms > mrun + kSlack;
-      const float mx = bump ? ms : mrun;
-      const float alpha = bump ? fast_exp2(mrun - mx) : 1.0f;
-      const float neg = mx != kNoScore ? -mx : 0.f;
       float l = lrun * alpha;
       uint32_t pk[2][8];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int pr = 0; pr < 8; ++pr) {
-          const float p0 = fast_exp2(RAW ? fmaf(sc[kb][2 * pr], a.qscale, neg) : sc[kb][2 * pr] + neg);
-          const float p1 = fast_exp2(RAW ? fmaf(sc[kb][2 * pr + 1], a.qscale, neg) : sc[kb][2 * pr + 1] + neg);
+          const float s0 = sc[kb][2 * pr], s1 = sc[kb][2 * pr + 1];
+          const float p0 = fast_exp2(RAW ? fmaf(s0, a.qscale, neg) : FIXED ? s0 : s0 + neg);
+          const float p1 = fast_exp2(RAW ? fmaf(s1, a.qscale, neg) : FIXED ? s1 : s1 + neg);
           // P enters its product rounded to bf16 (half a step, 2^-9 of a
           // probability); the sum keeps the fp32 values
           pk[kb][pr] = pack_bf16x2(p0, p1);
@@ -349,12 +379,14 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
         }
       // (the test on l, true for every finite sum, keeps this branch behind
       // the block above, whose exponentials run under the score products)
-      const bool rescale = __builtin_amdgcn_ballot_w64(bump && mrun != kNoScore && l >= 0.f) != 0;
       lrun = l;
-      mrun = mx;
-      if (__builtin_expect(rescale, 0)) {
+      if constexpr (!FIXED) {
+        const bool rescale = __builtin_amdgcn_ballot_w64(bump && mrun != kNoScore && l >= 0.f) != 0;
+        mrun = mx;
+        if (__builtin_expect(rescale, 0)) {
 #pragma unroll
-        for (int ob = 0; ob < NOB; ++ob) oacc[ob] = oacc[ob] * alpha;
+          for (int ob = 0; ob < NOB; ++ob) oacc[ob] = oacc[ob] * alpha;
+        }
       }
       // O^T += V^T P^T: k-step j takes keys 16 (j % 2) + {0..3, 8..11} + 4 lh of key block j / 2
       const uint8_t *const vt = cur + TILE;
@@ -463,29 +495,32 @@ __global__ __launch_bounds__(256) void k_attend_chunk_combine(AttendArgs a) {
 hipError_t launch_attend_chunk(const Shape &s, const AttendCall &c, const AttendArgs &a, hipStream_t st) {
   const AttendPlan &p = *c.plan;
   const dim3 grid(p.pre_tiles * s.nkv);
-#define EB_CHUNK(HD_, F8_)                                                                                     \
-  do {                                                                                                         \
-    if (c.softcap > 0.f && c.slopes)                                                                           \
-      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, true, true>), grid, dim3(256), 0, st, a);                   \
-    else if (c.softcap > 0.f)                                                                                  \
-      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, true, false>), grid, dim3(256), 0, st, a);                  \
-    else if (c.slopes)                                                                                         \
-      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, false, true>), grid, dim3(256), 0, st, a);                  \
-    else                                                                                                       \
-      hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, false, false>), grid, dim3(256), 0, st, a);                 \
-  } while (0)
+  const int mode = c.slopes ? (c.softcap > 0.f ? kCapBiased : kBiased)
+                            : (c.softcap > kCappedMost ? kCapBiased : c.softcap > 0.f ? kCapped : kPlain);
+#define EB_CHUNK_M(HD_, F8_, MODE_)                                                        \
+  case MODE_:                                                                              \
+    hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, MODE_>), grid, dim3(256), 0, st, a);      \
+    break
+#define EB_CHUNK(HD_, F8_)             \
+  switch (mode) {                      \
+    EB_CHUNK_M(HD_, F8_, kPlain);      \
+    EB_CHUNK_M(HD_, F8_, kCapped);     \
+    EB_CHUNK_M(HD_, F8_, kBiased);     \
+    EB_CHUNK_M(HD_, F8_, kCapBiased);  \
+  }
   if (s.hd == 128) {
-    if (a.kv.f8)
-      EB_CHUNK(128, true);
-    else
-      EB_CHUNK(128, false);
+    if (a.kv.f8) {
+      EB_CHUNK(128, true)
+    } else {
+      EB_CHUNK(128, false)
+    }
+  } else if (a.kv.f8) {
+    EB_CHUNK(64, true)
   } else {
-    if (a.kv.f8)
-      EB_CHUNK(64, true);
-    else
-      EB_CHUNK(64, false);
+    EB_CHUNK(64, false)
   }
 #undef EB_CHUNK
+#undef EB_CHUNK_M
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (p.pre_comb_rows > 0) {

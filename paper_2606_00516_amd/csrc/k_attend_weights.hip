@@ -3,13 +3,18 @@
 // with the rows' log-sum-exp from the attention that ran before.
 //
 // The same scores again, key by key instead of row by row, so that each
-// weight is one lane's register sum and no atomics are needed: a block takes
-// 128 keys of a (request, kv head), each of its four wavefronts holds 32 keys'
-// K in registers as the A operand, and the rows stream by in tiles of 64
-// (64 / G positions) through two LDS buffers.  Per 32 x 32 scores 8 products of
-// 32 cycles stand against 16 exponentials, multiply-adds and sums per lane
-// (about 28 cycles each, 70 with the cap): bound by the vector unit.
+// weight is one lane's register sum and no atomics are needed.  A block takes
+// 64 keys of a (request, kv head), held by each of its four wavefronts as two
+// 32-key A operands; the wavefronts take every fourth run of 32 rows (32 / G
+// positions x G heads), loaded straight into registers one run ahead: no LDS
+// and no barrier on the walk, whose length is that of the block whose keys
+// the most rows see (six prompts of about 1800 rows in documents of 300, hd 64:
+// 96 us through LDS tiles that the block shared, 56 so).  Per 32 x 64 scores 2 hd / 16 products of 32
+// cycles stand against 32 exponentials, multiply-adds and sums per lane
+// (about 26 cycles each, 70 with the cap): bound by the vector unit.
 #include <string.h>
+
+#include <cmath>
 
 #include "attend_device.h"
 
@@ -17,14 +22,11 @@ namespace eb {
 
 namespace {
 
-constexpr int kWaves = 4, kRT = 64;  // rows per tile
+constexpr int kWaves = 4;
 
 template <int HD, bool F8, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
-  constexpr int ROW = HD * 2, CPR = ROW / 16, TILE = kRT * ROW;
-  constexpr int NKS = HD / 16;
-  constexpr int RPI = 1024 / ROW, NI = kRT / (RPI * kWaves);  // rows per load instruction, instructions per wave
-  __shared__ __attribute__((aligned(16))) uint8_t buf[2 * TILE];
+  constexpr int NKS = HD / 16, KG = kWeightKeys / 32;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, lh = lane >> 5;
@@ -34,130 +36,189 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
   const auto field = [&](int f) { return __builtin_amdgcn_readfirstlane(m[f * a.n + k]); };
   const int seq = field(PRE_SEQ), row0 = field(PRE_ROW), c = field(PRE_CTX), n = field(PRE_LEN),
             prefix = field(PRE_PREFIX);
-  const int klen = c + n, G = a.group, PB = kRT / G;  // positions per tile
+  const int klen = c + n, G = a.group, PB = 32 / G;  // positions per run
   const int j0 = a.weight_rows > 0 ? max(0, n - a.weight_rows) : 0;
   const int first = min(c, attend_first(c + j0, a.window)) / kWeightKeys;
-  const int kb0 = (first + blk - field(PRE_WBLOCK0)) * kWeightKeys;  // the block's first key
-  const int k0 = kb0 + wave * 32;                                         // this wavefront's
+  const int k0 = (first + blk - field(PRE_WBLOCK0)) * kWeightKeys;  // the block's first key
   const int cols = (a.nq + 2 * a.nkv) * HD;
 
-  // K of the wavefront's 32 keys: lane (lq, lh) holds dims 16 ks + 8 lh .. of key lq
-  u32x4_t kf[NKS];
-  {
-    const int key = min(k0 + lq, klen - 1);
-    const int phys = a.kv.bt[(size_t)seq * a.kv.max_pages + key / kPageSize];
-    const bool ok = (unsigned)phys < (unsigned)a.kv.num_pages && k0 + lq < klen;
-    const size_t e0 = (((size_t)(ok ? phys : 0) * a.nkv + kh) * kPageSize + key % kPageSize) * HD + 8 * lh;
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) {
-      u32x4_t v;
-      if constexpr (F8)
-        v = e4m3x8_to_bf16x8(*reinterpret_cast<const u32x2_t *>(a.kv.k8() + e0 + ks * 16));
-      else
-        v = ld_u32x4(a.kv.k + e0 + ks * 16);
-      kf[ks] = ok ? v : u32x4_t{0u, 0u, 0u, 0u};
-    }
-  }
   // rows that may see the block's keys: from the first position at or past
   // its first key (all of them below a prefix), up to the window's reach
-  int ja = kb0 < prefix ? j0 : max(j0, kb0 - c);
+  int ja = k0 < prefix ? j0 : max(j0, k0 - c);
   int jb = n;
-  if (a.window > 0) jb = min(n, max(0, kb0 + kWeightKeys - 1 + a.window - c));
-  ja = ja / PB * PB;
-  const int ntiles = ja < jb ? (jb - ja + PB - 1) / PB : 0;
-
-  // row rr of a tile is position rr / G, head rr % G; load instruction i of
-  // wave w fills rows RPI (i 4 + w) .. + RPI - 1, chunk ch of row rr at ch ^ (rr & 7)
-  auto dma = [&](int t, uint8_t *dst) {
-    const int pos = ja + t * PB;  // uniform
-    const int left = n - pos;     // positions that exist
-    const uint16_t *base = a.qkv + (size_t)(row0 + pos) * cols + (size_t)kh * G * HD;
-    // (the range ends with the last row's last head of the group)
-    const int bytes =
-        __builtin_amdgcn_readfirstlane(left > 0 ? ((min(left, PB) - 1) * cols + G * HD) * 2 : 0);
-    const buf_rsrc_t rs = make_rsrc(base, bytes);
+  if (a.window > 0) jb = min(n, max(0, k0 + kWeightKeys - 1 + a.window - c));
+  if (a.first_key) {
+    // documents: only rows from the first to the last that sees one of the
+    // block's keys are worth their products
+    __shared__ int span[2];
+    if (tid < 2) span[tid] = tid ? 0 : 0x7fffffff;
+    __syncthreads();
+    int mn = 0x7fffffff, mx = 0;
+    for (int j = ja + tid; j < jb; j += 8 * 256) {
+      int f[8];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int rr0 = RPI * (i * kWaves + wave), rr = rr0 + lane / CPR, ch = (lane % CPR) ^ (rr & 7);
-      lds_dma16(rs, dst + rr0 * ROW, (uint32_t)(((rr / G) * cols + (rr % G) * HD) * 2 + 16 * ch));
+      for (int u = 0; u < 8; ++u) f[u] = a.first_key[row0 + min(j + 256 * u, n - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int ju = j + 256 * u;
+        if (ju < jb && f[u] < min(k0 + kWeightKeys, max(c + ju + 1, prefix))) {
+          mn = min(mn, ju);
+          mx = max(mx, ju + 1);
+        }
+      }
     }
-  };
-  float acc[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-  int qaddr[4];
+    for (int o = 32; o >= 1; o >>= 1) {
+      mn = min(mn, __shfl_xor(mn, o, 64));
+      mx = max(mx, __shfl_xor(mx, o, 64));
+    }
+    if (lane == 0) {
+      atomicMin(&span[0], mn);
+      atomicMax(&span[1], mx);
+    }
+    __syncthreads();
+    ja = max(ja, __builtin_amdgcn_readfirstlane(span[0]));
+    jb = min(jb, __builtin_amdgcn_readfirstlane(span[1]));
+  }
+  const int runs = ja < jb ? (jb - ja + PB - 1) / PB : 0;
+
+  float acc[KG][16];
 #pragma unroll
-  for (int k4 = 0; k4 < 4; ++k4) qaddr[k4] = lq * ROW + 16 * ((2 * k4 + lh) ^ (lq & 7));
-  // bounds and log-sum-exp (log2 units) of this lane's row in each half of a tile
-  auto row_of = [&](int t, int half, int &rlo, int &rhi, int &pos, float &z, float &slope) {
-    const int rr = half * 32 + lq, j = ja + t * PB + rr / G, h = kh * G + rr % G;
-    const bool ok = j >= j0 && j < jb;
-    const int row = row0 + (ok ? j : 0);
-    pos = c + j;
-    rlo = ok ? row_first(a, row, pos) : 0;
-    rhi = ok ? max(pos + 1, prefix) : 0;
-    z = ok ? a.lse[(size_t)row * a.nq + h] * kLog2e : 0.f;
-    if constexpr (BIAS) slope = a.slopes[h] * kLog2e;
-  };
-  if (ntiles > 0) dma(0, buf);
-  wait_loads<0>();
-  __syncthreads();
-  for (int t = 0; t < ntiles; ++t) {
-    uint8_t *const cur = buf + (t & 1) * TILE;
-    if (t + 1 < ntiles) dma(t + 1, buf + ((t + 1) & 1) * TILE);
+  for (int g = 0; g < KG; ++g)
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      int rlo, rhi, pos;
-      float z, slope = 0.f;
-      row_of(t, half, rlo, rhi, pos, z, slope);
-      // nothing of the wavefront's keys visible to any of the 32 rows
-      if (__builtin_amdgcn_ballot_w64(rlo < k0 + 32 && rhi > k0 && rlo < rhi) == 0) continue;
-      f32x16_t s;
+    for (int i = 0; i < 16; ++i) acc[g][i] = 0.f;
+  if (wave < runs) {
+    // K of the block's keys: lane (lq, lh) holds dims 16 ks + 8 lh .. of key 32 g + lq
+    u32x4_t kf[KG][NKS];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int g = 0; g < KG; ++g) {
+      const int key = min(k0 + 32 * g + lq, klen - 1);
+      const int phys = a.kv.bt[(size_t)seq * a.kv.max_pages + key / kPageSize];
+      const bool ok = (unsigned)phys < (unsigned)a.kv.num_pages && k0 + 32 * g + lq < klen;
+      const size_t e0 = (((size_t)(ok ? phys : 0) * a.nkv + kh) * kPageSize + key % kPageSize) * HD + 8 * lh;
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
-        const u32x4_t q = *reinterpret_cast<const u32x4_t *>(cur + half * 32 * ROW + qaddr[ks & 3] + 128 * (ks >> 2));
-        s = mfma32x32x16(kf[ks], q, s);
-      }
-      const bool masked = __builtin_amdgcn_ballot_w64(rlo > k0 || rhi < k0 + 32) != 0;
-      const float d0 = (float)(pos - k0 - 4 * lh);
-      const int d = k0 + 4 * lh - rlo;
-      const unsigned span = (unsigned)max(rhi - rlo, 0);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int at = 8 * (i >> 2) + (i & 3);
-        float p;
-        if constexpr (CAP || BIAS) {
-          float v = mod_score<CAP>(s[i], a.qscale, a.cap2);
-          if constexpr (BIAS) v = fmaf(-slope, fabsf(d0 - (float)at), v);
-          p = fast_exp2(v - z);
-        } else {
-          p = fast_exp2(fmaf(s[i], a.qscale, -z));
-        }
-        if (masked) p = (unsigned)(d + at) < span ? p : 0.f;
-        acc[i] += p;
+        u32x4_t v;
+        if constexpr (F8)
+          v = e4m3x8_to_bf16x8(*reinterpret_cast<const u32x2_t *>(a.kv.k8() + e0 + ks * 16));
+        else
+          v = ld_u32x4(a.kv.k + e0 + ks * 16);
+        kf[g][ks] = ok ? v : u32x4_t{0u, 0u, 0u, 0u};
       }
     }
-    wait_loads<0>();
-    __syncthreads();
-  }
-  // over the 32 rows' lanes; lane lq keeps value lq % 16
-  float mine = 0.f;
+    // Row lq of a run is position lq / G, head lq % G: its q as the B operand,
+    // its visible keys [lo, lo + span) and its log-sum-exp in log2 units.
+    // Runs past the end read the last row and see nothing.
+    const int jr = lq / G, head = kh * G + lq - jr * G;
+    const uint16_t *const qh = a.qkv + (size_t)row0 * cols + (size_t)head * HD + 8 * lh;
+    float slope = 0.f;
+    if constexpr (BIAS) slope = a.slopes[head] * kLog2e;
+    struct Run {
+      u32x4_t q[NKS];
+      float lse;
+      int first;
+    };
+    auto load = [&](int t, Run &r) {
+      const int j = min(ja + t * PB + jr, n - 1);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float v = acc[i];
+      for (int ks = 0; ks < NKS; ++ks) r.q[ks] = ld_u32x4(qh + (size_t)j * cols + ks * 16);
+      r.lse = a.lse[(size_t)(row0 + j) * a.nq + head];
+      r.first = a.first_key ? a.first_key[row0 + j] : 0;
+    };
+    auto add = [&](int t, const Run &r) {
+      const int j = ja + t * PB + jr, pos = c + j;
+      const bool ok = j < jb;
+      int lo = max(r.first, 0);
+      if (a.window > 0) lo = max(lo, pos - a.window + 1);
+      const int span = ok ? max(max(pos + 1, prefix) - lo, 0) : 0;
+      const int d = k0 - lo;  // the block's first key from the row's
+      // nothing of the block's keys visible to any of the 32 rows
+      if (__builtin_amdgcn_ballot_w64(span > 0 && d + kWeightKeys > 0 && d < span) == 0) return;
+      const bool masked = __builtin_amdgcn_ballot_w64(d < 0 || d + kWeightKeys > span) != 0;
+      const float z = r.lse * kLog2e;
+      const int dl = d + 4 * lh;
+      const float d0 = BIAS ? (float)(pos - k0 - 4 * lh) : 0.f;
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) v += shfl_xor_f32(v, o);
-    mine = (lq & 15) == i ? v : mine;
+      for (int g = 0; g < KG; ++g) {
+        f32x16_t one[1];
+        f32x16_t &s = one[0];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) s = mfma32x32x16(kf[g][ks], r.q[ks], s);
+        if constexpr (CAP) {
+          if (all_small<1>(one, a)) {
+            asm volatile("");  // (a branch: not both forms and a select)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = small_score(s[i], a);
+          } else {
+            asm volatile("");
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = mod_score<true>(s[i], a.qscale, a.cap2);
+          }
+        }
+        if constexpr (CAP || BIAS) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float v = CAP ? s[i] : s[i] * a.qscale;
+            if constexpr (BIAS) v = fmaf(-slope, fabsf(d0 - (float)(32 * g + 8 * (i >> 2) + (i & 3))), v);
+            s[i] = v - z;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], a.qscale, -z);
+        }
+        if (masked) {
+          asm volatile("");  // (a branch, not 16 selects in every run)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            s[i] = (unsigned)(dl + 32 * g + 8 * (i >> 2) + (i & 3)) < (unsigned)span ? s[i] : kNoScore;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[g][i] += s[i];
+      }
+    };
+    Run x, y;
+    load(wave, x);
+    for (int t = wave; t < runs; t += 2 * kWaves) {
+      load(t + kWaves, y);
+      add(t, x);
+      load(t + 2 * kWaves, x);
+      add(t + kWaves, y);
+    }
   }
-  if (lq < 16) {
-    const int key = k0 + 8 * (lq >> 2) + 4 * lh + (lq & 3);
+  // Over the 32 rows' lanes by halves: in each exchange a lane keeps the half
+  // of its values that its own bit names and adds the partner's of that half
+  // (31 exchanges instead of 5 for each of 32 values); lane lq ends with value
+  // lq.  Then over the wavefronts in their order.
+  __shared__ float part[kWaves][kWeightKeys];
+  float v[16 * KG];
+#pragma unroll
+  for (int i = 0; i < 16 * KG; ++i) v[i] = acc[i / 16][i % 16];
+  static_assert(KG == 2, "as many values as lanes of a half wavefront");
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) {
+    const bool up = (lq & o) != 0;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float give = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+      v[i] = keep + shfl_xor_f32(give, o);
+    }
+  }
+  part[wave][32 * (lq >> 4) + 8 * ((lq >> 2) & 3) + 4 * lh + (lq & 3)] = v[0];
+  __syncthreads();
+  if (tid < kWeightKeys) {
+    const int key = k0 + tid;
     if (key < klen) {
       const int phys = a.kv.bt[(size_t)seq * a.kv.max_pages + key / kPageSize];
       if ((unsigned)phys < (unsigned)a.kv.num_pages) {
+        float got = part[0][tid];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) got += part[w][tid];
         float *dst = a.weights + ((size_t)phys * a.nkv + kh) * kPageSize + key % kPageSize;
-        *dst = key < c ? *dst + mine : mine;  // a new key starts at what this call gives it
+        *dst = key < c ? *dst + got : got;  // a new key starts at what this call gives it
       }
     }
   }
@@ -231,6 +292,17 @@ hipError_t launch_attend(const Shape &s, const AttendCall &c, hipStream_t st) {
   const float scale = c.scale * (c.kv.f8 ? c.kv.ks : 1.f);
   a.qscale = c.softcap > 0.f ? 2.f * kLog2e * (scale / c.softcap) : kLog2e * scale;
   a.cap2 = c.softcap * kLog2e;
+  if (c.softcap > 0.f) {
+    constexpr double k[5] = {0.999998495, -0.333269731, 0.132574549, -0.0501952578, 0.0131941869};
+    const double y = (double)scale / c.softcap;
+    double f = (double)c.softcap * 1.4426950408889634 * y;
+    bool ok = true;
+    for (int i = 0; i < 5; ++i, f *= y * y) {
+      a.tanh_c[i] = (float)(f * k[i]);
+      ok = ok && std::fabs(a.tanh_c[i]) > 1e-36f && std::fabs(a.tanh_c[i]) < 1e36f;
+    }
+    a.small_raw = ok ? (float)(0.7 / y) : 0.f;
+  }
   hipError_t e = hipSuccess;
   if (p.n_dec > 0) {
     e = with_table(a, p.dec, p.n_dec, c.ws + p.o_dec, st);

@@ -30,7 +30,7 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   }
   const auto keys_of = [&](int i) { return b.context_lens_host[i] + b.chunk_lens_host[i]; };
   p.n_dec = (int32_t)ones.size();
-  p.dec.assign((size_t)DEC_FIELDS * p.n_dec + 1, 0);
+  p.dec.assign((size_t)DEC_FIELDS * p.n_dec, 0);
   int64_t runs = 0;
   for (int32_t d = 0; d < p.n_dec; ++d) {
     const int i = ones[d];
@@ -53,7 +53,7 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   }
   std::stable_sort(many.begin(), many.end(), [&](int32_t x, int32_t y) { return keys_of(x) > keys_of(y); });
   p.n_pre = (int32_t)many.size();
-  p.pre.assign((size_t)PRE_FIELDS * p.n_pre + 1, 0);
+  p.pre.assign((size_t)PRE_FIELDS * p.n_pre, 0);
   int32_t part = p.dec_splits;
   for (int32_t k = 0; k < p.n_pre; ++k) {
     const int i = many[k];
@@ -105,6 +105,46 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   p.o_part_ml = take((size_t)part * cfg.n_q_heads * 8);
   p.o_scores = take((size_t)runs * 64);
   p.total = off;
+}
+
+bool plan_evict(int32_t n_kv, int32_t S, const int32_t *lens, const int32_t *keep, EvictPlan &p) {
+  p = EvictPlan();
+  p.S = S;
+  p.words.assign((size_t)EV_FIELDS * S, 0);
+  int64_t runs = 0;
+  for (int i = 0; i < S; ++i) {
+    const int32_t c = lens[i], k = std::min(lens[i], keep[i]);
+    const size_t n = (size_t)S;
+    p.words[EV_LEN * n + i] = c;
+    p.words[EV_KEEP * n + i] = keep[i];
+    p.words[EV_GROUP0 * n + i] = (int32_t)p.groups;
+    p.words[EV_SEG0 * n + i] = (int32_t)p.segments;
+    p.words[EV_LIST0 * n + i] = (int32_t)runs;
+    p.groups += (k + kEvictGroupKeys - 1) / kEvictGroupKeys;
+    p.segments += (c + evict_segment(c) - 1) / evict_segment(c);
+    runs += (c + 15) / 16;
+    p.max_len = std::max(p.max_len, c);
+    p.max_keep = std::max(p.max_keep, k);
+    if (p.groups * n_kv > 0x7FFFFFFF || p.segments * n_kv > 0x7FFFFFFF || runs > 0x7FFFFFFF) return false;
+  }
+  size_t off = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off = (off + bytes + 255) / 256 * 256;
+    return o;
+  };
+  const size_t heads = (size_t)S * n_kv;
+  p.o_words = take(p.words.size() * 4);
+  p.o_kept = take(heads * p.max_keep * 4);
+  if (p.max_len > kEvictBlock) {
+    p.o_hist = take(heads * 2049 * 4);
+    p.o_list_v = take((size_t)runs * 16 * n_kv * 4);
+    p.o_list_t = take((size_t)runs * 16 * n_kv * 4);
+    p.o_seg = take((size_t)p.segments * n_kv * 8);
+    p.o_solved = take(heads * 8);
+  }
+  p.total = off;
+  return true;
 }
 
 }  // namespace eb

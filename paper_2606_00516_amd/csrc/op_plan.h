@@ -11,7 +11,7 @@ namespace eb {
 
 constexpr int kAttendTile = 64;    // keys per step of a chunk's rows
 constexpr int kAttendRows = 128;   // query rows (positions x heads of the group) per block
-constexpr int kWeightKeys = 128;   // keys per block of the weights pass of a chunk
+constexpr int kWeightKeys = 64;    // keys per block of the weights pass of a chunk
 constexpr int kWeightSpan = 1024;  // keys per block of the weights pass of a decode row
 
 // Keys per split of a decode row that sees `keys` of them, a multiple of the
@@ -27,7 +27,7 @@ __host__ __device__ inline int32_t attend_first(int32_t p, int32_t window) {
 
 // Tables of one attention call.  Decode part: requests with one new row, in
 // batch order; chunk part: the others, the most keys first.  Each table is a
-// run of arrays (below) of n entries, then one closing word.
+// run of arrays (below) of n entries.
 struct AttendPlan {
   int32_t T = 0;
   int32_t n_dec = 0, dec_splits = 0, dec_wblocks = 0;
@@ -54,5 +54,28 @@ enum PreField {
 // check_batch.
 void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
                  int32_t weight_rows, AttendPlan &p);
+
+// ---- eviction ----
+constexpr int kEvictFew = 512;         // keys of the longest request: one wavefront chooses
+constexpr int kEvictBlock = 16384;     // one block chooses; longer: segments
+constexpr int kEvictSegment = 4096, kEvictSegments = 512;
+constexpr int kEvictGroupKeys = 64;    // kept keys per copy block
+// Keys per segment of a request of c keys: at most kEvictSegments of them.
+__host__ __device__ inline int32_t evict_segment(int32_t c) {
+  const int32_t all = kEvictSegment * kEvictSegments;
+  return kEvictSegment * ((c + all - 1) / all > 1 ? (c + all - 1) / all : 1);
+}
+
+// length, kept, first copy block, first segment, first 16-key run of the lists
+enum EvictField { EV_LEN = 0, EV_KEEP, EV_GROUP0, EV_SEG0, EV_LIST0, EV_FIELDS };
+struct EvictPlan {
+  int32_t S = 0, max_len = 0, max_keep = 0;
+  int64_t groups = 0, segments = 0;
+  std::vector<int32_t> words;
+  size_t o_words = 0, o_kept = 0, o_hist = 0, o_list_v = 0, o_list_t = 0, o_seg = 0, o_solved = 0, total = 0;
+};
+// Lengths as given (not negative, at most 2^30).  False: more blocks than a
+// launch holds.
+bool plan_evict(int32_t n_kv, int32_t S, const int32_t *lens, const int32_t *keep, EvictPlan &p);
 
 }  // namespace eb

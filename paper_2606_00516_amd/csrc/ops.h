@@ -46,10 +46,9 @@ struct EvictCall {
   const float *weights;
   float *dst_weights;
   int32_t *kept;
-  int32_t S, sink, recent, kept_stride;
-  int32_t max_len;
-  long groups;  // destination page groups over all requests
-  Table table;
+  int32_t sink, recent, kept_stride;
+  const EvictPlan *plan;
+  char *ws;
 };
 hipError_t launch_evict(const Shape &s, const EvictCall &c, hipStream_t st);
 
