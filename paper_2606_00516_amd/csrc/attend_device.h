@@ -6,6 +6,8 @@
 //   max(first_key, p - window + 1, 0) <= t < max(p + 1, prefix).
 // Scores are held in log2 units.
 #pragma once
+#include <type_traits>
+
 #include "attention_tiles.h"
 #include "op_meta.h"
 #include "ops.h"
@@ -77,17 +79,53 @@ EB_DEV void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
 }
 
+// A buffer range (uniform) as the four words of its descriptor.
+EB_DEV u32x4_t range_words(const uint8_t *base, int bytes) {
+  const uint64_t b = (uint64_t)base;
+  auto u = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+  return u32x4_t{u((uint32_t)b), u((uint32_t)(b >> 32) & 0xFFFFu), u((uint32_t)bytes), 0x00020000u};
+}
+// One 16-byte-per-lane load from a buffer range (uniform) straight into LDS:
+// lane l fills bytes 16 l .. 16 l + 15 from byte address dst (uniform) with the
+// bytes at its offset, zeros past the range.  It has no output register, and
+// the compiler does not count it: wait_loads before the bytes are read.  (The
+// counted form makes the compiler wait for all of them before any read of the
+// same array, the loads of later tiles among them.)  It sets m0, which no
+// instruction around it keeps a value in.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+template <bool ONCE = false>
+EB_DEV void lds_fill16(u32x4_t range, uint32_t dst, uint32_t off) {
+  if constexpr (ONCE)  // data read once
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+                 :
+                 : "s"(dst), "v"(off), "s"(range)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(dst), "v"(off), "s"(range)
+                 : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// Byte address of a __shared__ array for it.
+EB_DEV uint32_t lds_at(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // Joins ns partials (entries base, base + nq, ..) into row entry `at` of out
-// and lse, by one wavefront: lane s % 64 holds partial s's factor, HD / 64 output
-// dims per lane, eight partials' loads issued together.
+// and lse, by one wavefront: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.
+// Lane s % 64 holds partial s's factor, HD / 64 output dims per lane; up to 16
+// partials' loads are issued together.
 template <int HD>
 EB_DEV void join_splits(const AttendArgs &a, size_t base, int ns, size_t at, bool empty, int lane) {
   constexpr int DPL = HD / 64;
   const size_t stride = (size_t)a.nq;
+  const float *po = a.part_o + base * HD + lane * DPL, *pm = a.part_ml + base * 2;
   float mx = kNoScore;
-  for (int s = lane; s < ns; s += 64) mx = fmaxf(mx, a.part_ml[(base + s * stride) * 2]);
+  for (int s = lane; s < ns; s += 64) mx = fmaxf(mx, pm[s * stride * 2]);
   mx = wave_max(mx);
   float den = 0.f, acc[DPL];
 #pragma unroll
@@ -96,26 +134,29 @@ EB_DEV void join_splits(const AttendArgs &a, size_t base, int ns, size_t at, boo
     const int s = c + lane;
     float f = 0.f;
     if (s < ns) {
-      const float ms = a.part_ml[(base + s * stride) * 2];
+      const float ms = pm[s * stride * 2];
       f = ms == kNoScore ? 0.f : fast_exp2(ms - mx);
-      if (f != 0.f) den += f * a.part_ml[(base + s * stride) * 2 + 1];
+      if (f != 0.f) den += f * pm[s * stride * 2 + 1];
     }
     const int n = min(64, ns - c);
-    for (int j = 0; j < n; j += 8) {
-      float o[8][DPL];
+    auto add = [&](int j, auto count) {
+      constexpr int N = decltype(count)::value;
+      float o[N][DPL];
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < N; ++u)
 #pragma unroll
-        for (int i = 0; i < DPL; ++i)
-          o[u][i] = j + u < n ? a.part_o[(base + (size_t)(c + j + u) * stride) * HD + lane * DPL + i] : 0.f;
+        for (int i = 0; i < DPL; ++i) o[u][i] = po[(size_t)min(c + j + u, ns - 1) * stride * HD + i];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < N; ++u) {
+        // (past the last split the factor is 0; a split that saw nothing wrote no outputs)
         const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j + u));
-        // (a split that saw nothing wrote no outputs)
 #pragma unroll
         for (int i = 0; i < DPL; ++i) acc[i] = w != 0.f ? fmaf(w, o[u][i], acc[i]) : acc[i];
       }
-    }
+    };
+    int j = 0;
+    for (; j + 8 < n; j += 16) add(j, std::integral_constant<int, 16>{});
+    if (j < n) add(j, std::integral_constant<int, 8>{});
   }
   den = wave_sum(den);
 #pragma unroll

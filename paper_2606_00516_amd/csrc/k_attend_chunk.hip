@@ -9,10 +9,12 @@
 // product.  Two LDS buffers of a K and a V tile (row-major, swizzled) are
 // filled by direct loads, K two tiles and V one tile ahead, so the scores of
 // tile t + 1 run on the matrix cores under the exponentials of tile t; 8-bit
-// tiles pass through registers to become bf16.  Per tile and wavefront 32
-// products of 32 cycles stand against 32 scores per lane: about 28 cycles of
-// vector work each, 70 with the cap (two more transcendentals of 16 cycles),
-// which makes capped attention bound by the vector unit.
+// tiles pass through registers to become bf16.  Per tile and wavefront (head
+// size 128) 32 products of 32 cycles, 1024 cycles, stand against 32 scores per
+// lane: some 45 cycles of vector work each, 1440, where the cap's polynomial
+// serves: the vector unit bounds capped attention.  4096 rows over 32768 keys,
+// 32 heads: 2.73 ms, 856 TFLOP/s; the counters put the matrix cores at 42 % and
+// the vector unit at 58 %, so the two wavefronts of a SIMD hardly overlap them.
 //
 // With few rows the keys are split over blocks (the plan's rule) and joined by
 // k_attend_chunk_combine.
@@ -33,7 +35,7 @@ constexpr float kSlack = 8.0f;
 struct PreReq {
   int k, seq, row0, c, n, prefix, nsplit;
 };
-__device__ __forceinline__ PreReq pre_req(const AttendArgs &a, const int32_t *m, int k) {
+__device__ __forceinline__ PreReq pre_req(const AttendArgs &a, meta_t m, int k) {
   PreReq r;
   r.k = k;
   // (uniform; said so, so that what follows from them stays in scalar registers)
@@ -45,8 +47,6 @@ __device__ __forceinline__ PreReq pre_req(const AttendArgs &a, const int32_t *m,
   r.nsplit = __builtin_amdgcn_readfirstlane(m[PRE_NSPLIT * a.n + k]);
   return r;
 }
-
-typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
 // How scores are made.  kCapped (no bias, a cap up to kCappedMost) needs no
 // running maximum: |s| <= 92 in log2 units keeps 2^s and sums of 2^30 of them
@@ -66,11 +66,10 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
   constexpr int NOB = HD / 32;       // 32-dim output blocks
   __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE];
   __shared__ int red[2], odd[2];
-  uint8_t *const buf0 = lds, *const buf1 = lds + 2 * TILE;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, lh = lane >> 5;
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int tile_id = blockIdx.x / a.nkv, kh = blockIdx.x - tile_id * a.nkv;
   const PreReq r = pre_req(a, m, last_at_or_below(m + PRE_TILE0 * a.n, a.n, tile_id));
   const int G = a.group, BQ = kAttendRows / G;
@@ -142,30 +141,44 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
   static_assert(PPT == 4, "tile = 4 pages");
   typedef const __attribute__((address_space(4))) int32_t *bt_ptr_t;
   const bt_ptr_t btc = (bt_ptr_t)bt;
-  auto bt_tile = [&](int t) -> i32x4_t {  // pages past the sequence repeat its last id (empty ranges below)
-    i32x4_t v;
+  constexpr int ES = F8 ? 1 : 2;
+  constexpr int KPI = 1024 / (HD * ES), NI = KT / (KPI * kWaves);  // keys of one load instruction of a wave; instructions of a tile
+  const uint32_t page_bytes = (uint32_t)(a.nkv * kPageSize * HD * ES);
+  const size_t head_at = (size_t)kh * (kPageSize * HD * ES);
+  const uint8_t *const kbase = reinterpret_cast<const uint8_t *>(a.kv.k) + head_at;
+  const uint8_t *const vbase = reinterpret_cast<const uint8_t *>(a.kv.v) + head_at;
+  // The page of each of this wave's instructions: its id, then where it starts
+  // and how many bytes of it lie below klen (none for an id outside the pool).
+  // Loads past the range give zeros, without traffic.  K and V of a tile are
+  // found alike, V one tile later: worked out once, for both.
+  struct Ids {
+    int id[NI];
+  };
+  struct Ranges {
+    uint64_t at[NI];
+    int bytes[NI];
+  };
+  auto page_of = [&](int i) { return (KPI * kWaves * i) / kPageSize + wave * KPI / kPageSize; };
+  auto page_ids = [&](int t) {  // pages past the sequence repeat its last id (their ranges are empty)
+    Ids v;
 #pragma unroll
-    for (int j = 0; j < PPT; ++j) v[j] = btc[min(t * PPT + j, npages - 1)];
+    for (int i = 0; i < NI; ++i) v.id[i] = btc[min(t * PPT + page_of(i), npages - 1)];
     return v;
   };
-  constexpr int ES = F8 ? 1 : 2;
-  constexpr uint32_t kHeadBytes = kPageSize * HD * ES;  // one page's block of a kv head
-  const uint64_t page_bytes = (uint64_t)a.nkv * kHeadBytes;
-  const uint8_t *const kbase = reinterpret_cast<const uint8_t *>(a.kv.k) + (size_t)kh * kHeadBytes;
-  const uint8_t *const vbase = reinterpret_cast<const uint8_t *>(a.kv.v) + (size_t)kh * kHeadBytes;
-  // page j of a tile as a buffer range over its keys below klen (empty for an
-  // id outside the pool): loads past it give zeros, without traffic
-  auto page_rsrc = [&](const uint8_t *base, const i32x4_t &btv, int j, int first_key) -> buf_rsrc_t {
-    const int phys = j == 0 ? btv[0] : j == 1 ? btv[1] : j == 2 ? btv[2] : btv[3];
-    const int rem = klen - first_key;
-    const bool live = (unsigned)phys < (unsigned)a.kv.num_pages && rem > 0;
-    const int range = __builtin_amdgcn_readfirstlane(live ? min(rem, kPageSize) * (HD * ES) : 0);
-    return make_rsrc(base + (uint64_t)(uint32_t)(live ? phys : 0) * page_bytes, range);
+  auto ranges = [&](int t, const Ids &v) {
+    Ranges g;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int keys = min(max(klen - (t * PPT + page_of(i)) * kPageSize, 0), kPageSize);
+      g.bytes[i] =
+          __builtin_amdgcn_readfirstlane((unsigned)v.id[i] < (unsigned)a.kv.num_pages ? keys * (HD * ES) : 0);
+      g.at[i] = (uint64_t)(uint32_t)v.id[i] * page_bytes;
+    }
+    return g;
   };
   // --- bf16: load instruction i of wave w fills keys KPI (i 4 + w) .. + KPI - 1
   // of a tile; lane l writes chunk position l % CPR of key .. + l / CPR.
   // K chunk c of key t lies at c ^ (t & 7), V chunk c at c ^ 2 (t & 3).
-  constexpr int KPI = 1024 / ROW, NI = KT / (KPI * kWaves);
   uint32_t koff[NI], voff[NI];
   if constexpr (!F8) {
 #pragma unroll
@@ -175,29 +188,25 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
       voff[i] = (uint32_t)((key % kPageSize) * ROW + 16 * (pos ^ (2 * (key & 3))));
     }
   }
-  auto dma = [&](int t, const i32x4_t &btv, uint8_t *dst, bool is_v) {
+  const uint32_t lds0 = lds_at(lds);
+  auto dma = [&](const Ranges &g, int at, bool is_v) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int key0 = KPI * (i * kWaves + wave), j = key0 / kPageSize;
-      lds_dma16(page_rsrc(is_v ? vbase : kbase, btv, j, t * KT + j * kPageSize), dst + key0 * ROW,
-                is_v ? voff[i] : koff[i]);
-    }
+    for (int i = 0; i < NI; ++i)
+      lds_fill16(range_words((is_v ? vbase : kbase) + g.at[i], g.bytes[i]),
+                 lds0 + at + KPI * (i * kWaves + wave) * ROW, is_v ? voff[i] : koff[i]);
   };
   // --- 8 bits: unit u = tid + 256 i is 16 codes of key u / (HD / 16); they become two chunks
-  constexpr int CU = HD / 16, NF = KT * CU / 256;
-  u32x4_t kreg[F8 ? NF : 1], vreg[F8 ? NF : 1];
-  auto fetch = [&](int t, const i32x4_t &btv, u32x4_t (&reg)[F8 ? NF : 1], bool is_v) {
+  constexpr int CU = HD / 16;
+  u32x4_t kreg[F8 ? NI : 1], vreg[F8 ? NI : 1];
+  auto fetch = [&](const Ranges &g, u32x4_t (&reg)[F8 ? NI : 1], bool is_v) {
 #pragma unroll
-    for (int i = 0; i < (F8 ? NF : 0); ++i) {
-      const int key = (tid + 256 * i) / CU;
-      const int j = __builtin_amdgcn_readfirstlane(key / kPageSize);  // 64 / CU keys of one page per wavefront
-      reg[i] = buf_ld_u32x4<0>(page_rsrc(is_v ? vbase : kbase, btv, j, t * KT + j * kPageSize),
-                               (key % kPageSize) * HD + (tid % CU) * 16);
-    }
+    for (int i = 0; i < (F8 ? NI : 0); ++i)
+      reg[i] = buf_ld_u32x4<0>(make_rsrc((is_v ? vbase : kbase) + g.at[i], g.bytes[i]),
+                               ((tid + 256 * i) / CU % kPageSize) * HD + (tid % CU) * 16);
   };
-  auto land = [&](const u32x4_t (&reg)[F8 ? NF : 1], uint8_t *dst, bool is_v) {
+  auto land = [&](const u32x4_t (&reg)[F8 ? NI : 1], uint8_t *dst, bool is_v) {
 #pragma unroll
-    for (int i = 0; i < (F8 ? NF : 0); ++i) {
+    for (int i = 0; i < (F8 ? NI : 0); ++i) {
       const int key = (tid + 256 * i) / CU, ch = 2 * (tid % CU);
       const int x = is_v ? 2 * (key & 3) : key & 7;
       st_u32x4(dst + key * ROW + 16 * (ch ^ x), e4m3x8_to_bf16x8(u32x2_t{reg[i][0], reg[i][1]}));
@@ -265,30 +274,33 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
   if (t0 < t1) {
     if (tid < 2) odd[tid] = 0;
     f32x16_t sc[2];
-    i32x4_t bt1 = bt_tile(t0 + 1), bt2 = bt_tile(t0 + 2);
+    const Ids i0 = page_ids(t0), i1 = page_ids(t0 + 1);
+    Ids next = page_ids(t0 + 2);
+    Ranges vat = ranges(t0 + 1, i1);
     {
-      const i32x4_t b0 = bt_tile(t0);
+      const Ranges g0 = ranges(t0, i0);
       if constexpr (F8) {
-        u32x4_t k1[NF];
-        fetch(t0, b0, kreg, false);
-        fetch(t0, b0, vreg, true);
-        fetch(t0 + 1, bt1, k1, false);
-        land(kreg, buf0, false);
-        land(vreg, buf0 + TILE, true);
-        land(k1, buf1, false);
+        u32x4_t k1[NI];
+        fetch(g0, kreg, false);
+        fetch(g0, vreg, true);
+        fetch(vat, k1, false);
+        land(kreg, lds, false);
+        land(vreg, lds + TILE, true);
+        land(k1, lds + 2 * TILE, false);
       } else {
-        dma(t0, b0, buf0, false);
-        dma(t0, b0, buf0 + TILE, true);
-        if (t0 + 1 < t1) dma(t0 + 1, bt1, buf1, false);
+        dma(g0, 0, false);
+        dma(g0, TILE, true);
+        if (t0 + 1 < t1) dma(vat, 2 * TILE, false);
       }
     }
     wait_loads<0>();
     __syncthreads();
-    scores(buf0, sc);
+    scores(lds, sc);
     __syncthreads();  // every wave past the scores of the first tile before K of the third refills its buffer
     auto step = [&](int t, auto lastconst) {
       constexpr bool LAST = decltype(lastconst)::value;
-      uint8_t *const cur = ((t - t0) & 1) ? buf1 : buf0, *const nxt = ((t - t0) & 1) ? buf0 : buf1;
+      const int at = ((t - t0) & 1) * (2 * TILE);
+      uint8_t *const cur = lds + at, *const nxt = lds + (2 * TILE - at);
       const int k0 = t * KT;
       f32x16_t scn[2];
       // (before the next loads are issued: its barrier would wait for them)
@@ -296,15 +308,16 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
       const bool odd_values = masked && clean(cur + TILE, t & 1);
       if constexpr (!LAST) {
         // K of tile t and V of tile t - 1 were read before the last barrier
+        const Ranges kat = ranges(t + 2, next);
         if constexpr (F8) {
-          fetch(t + 2, bt2, kreg, false);
-          fetch(t + 1, bt1, vreg, true);
+          fetch(kat, kreg, false);
+          fetch(vat, vreg, true);
         } else {
-          if (t + 2 < t1) dma(t + 2, bt2, cur, false);
-          dma(t + 1, bt1, nxt + TILE, true);
+          if (t + 2 < t1) dma(kat, at, false);
+          dma(vat, 2 * TILE - at + TILE, true);
         }
-        bt1 = bt2;
-        bt2 = bt_tile(t + 3);
+        vat = kat;
+        next = page_ids(t + 3);
       }
       auto hide = [&]() {  // keys outside the row's range
         asm volatile("");  // (a branch, not 32 selects in every tile)
@@ -319,7 +332,12 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
       // plain scores are hidden before the next tile's are formed, so that
       // nothing splits the run of products and exponentials below
       if (MODE == kPlain && masked) hide();
+      // Vector work goes before the other wavefront's products, which keep the
+      // matrix cores busy from few issued instructions (capped, as above: 2.73
+      // ms; without: 2.93).
+      __builtin_amdgcn_s_setprio(0);
       if constexpr (!LAST) scores(nxt, scn);
+      __builtin_amdgcn_s_setprio(2);
       if constexpr (CAP) {
         if (all_small<2>(sc, a)) {
           asm volatile("");  // (a branch: not both forms and a select)
@@ -390,6 +408,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
       }
       // O^T += V^T P^T: k-step j takes keys 16 (j % 2) + {0..3, 8..11} + 4 lh of key block j / 2
       const uint8_t *const vt = cur + TILE;
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int ob = 0; ob < NOB; ++ob) {
         f32x16_t acc = oacc[ob];
@@ -403,7 +422,18 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
         }
         oacc[ob] = acc;
       }
+      // The outputs are read by vector instructions next, in the branch below or
+      // behind the loop: the wait states that a product's result needs before
+      // that are put here, tied to the outputs.  Left to the compiler, a copy
+      // of the last outputs at the end of a block followed their product too
+      // closely and read old values.
+      auto settle = [&]() {
+#pragma unroll
+        for (int ob = 0; ob < NOB; ++ob) asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 3" : "+v"(oacc[ob]));
+      };
+      if constexpr (LAST) settle();
       if (__builtin_expect(odd_values, 0)) {
+        if constexpr (!LAST) settle();
         // the values that were set to zero, for the rows that see their keys:
         // a sum with one of them is what that value makes of it
         for (int key = max(k0, rlo); key < min(k0 + KT, rhi); ++key) {
@@ -474,20 +504,19 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
   }
 }
 
-// Joins the splits of the rows that have several, one wavefront per (row, head).
+// Joins the splits of the rows that have several, one wavefront per query head.
 template <int HD>
 __global__ __launch_bounds__(256) void k_attend_chunk_combine(AttendArgs a) {
-  const int32_t *m = meta_words(a);
-  const int lane = threadIdx.x & 63;
-  // (requests without splits share the next one's first row: the last entry
-  // at or below the row is a request that has splits, or the row's own)
+  const meta_t m = meta_words(a);
+  // (a request without splits has the first row of the one after it: the last
+  // entry at or below a row is that of a request that has splits)
   const PreReq r = pre_req(a, m, last_at_or_below(m + PRE_COMB0 * a.n, a.n, blockIdx.x));
   const int qh = blockIdx.y * 4 + (threadIdx.x >> 6);
   if (qh >= a.nq) return;
   const int j = blockIdx.x - m[PRE_COMB0 * a.n + r.k], p = r.c + j;
   const bool empty = row_first(a, r.row0 + j, p) >= max(p + 1, r.prefix);
   const size_t base = ((size_t)m[PRE_PART0 * a.n + r.k] + (size_t)j * r.nsplit) * a.nq + qh;
-  join_splits<HD>(a, base, r.nsplit, (size_t)(r.row0 + j) * a.nq + qh, empty, lane);
+  join_splits<HD>(a, base, r.nsplit, (size_t)(r.row0 + j) * a.nq + qh, empty, threadIdx.x & 63);
 }
 
 }  // namespace

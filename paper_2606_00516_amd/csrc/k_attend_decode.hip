@@ -6,17 +6,18 @@
 // HBM.  Its four wavefronts stream the split's pages w, w + 4, .. through
 // two LDS slots each (direct loads, no registers) with one page in flight
 // while another is worked on; at two blocks per CU that is 64 KiB in flight
-// per CU.  Scores are formed as S^T = K Q^T on 16x16x32 products (16 tokens x
+// per CU (64 rows over 2350 keys on average, 8 kv heads, bf16: 110 us, 5.6 TB/s;
+// 13 rows over 69000, 8 bits: 327 us, 5.6 TB/s).  Scores are formed as S^T = K Q^T on 16x16x32 products (16 tokens x
 // 16 columns, G of them heads; lane l holds tokens 4 (l / 16) .. + 3 of head
 // l % 16), so the cap, the bias and the mask cost 4 values per lane and page
 // whatever G is.  O^T += V^T P^T takes V^T by the transposing LDS read; 8-bit
 // pages become bf16 on the way and are transposed by a product with a 0/1
 // matrix, which is exact.
 //
-// Splits are joined by k_attend_combine; with weights, the scores are left
-// in the workspace (4 G bytes per key beside the 4 hd read) and
+// Splits are joined by k_attend_decode_combine; with weights, the scores are left
+// in the workspace (4 G bytes per key beside the 4 hd read: 110 -> 126 us) and
 // k_attend_decode_weights turns them into normalised weights once the rows'
-// log-sum-exp is known, instead of reading K a second time.
+// log-sum-exp is known (9 us), instead of reading K a second time.
 #include "attend_device.h"
 
 namespace eb {
@@ -28,7 +29,7 @@ constexpr int kWaves = 4;
 struct DecRow {
   int d, seq, row, ctx, first, nkeys;  // first: first key streamed (of a whole page); nkeys = ctx + 1
 };
-__device__ __forceinline__ DecRow dec_row(const AttendArgs &a, const int32_t *m, int d) {
+__device__ __forceinline__ DecRow dec_row(const AttendArgs &a, meta_t m, int d) {
   DecRow r;
   // (uniform; said so, so that what follows from them stays in scalar registers)
   r.d = d;
@@ -54,15 +55,13 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
   constexpr int NKS = HD / 32, NOB = HD / 16, MAXG = 8;
   constexpr int ARRAY = kWaves * Tr::SLOT;
   static_assert(kWaves * MAXG * HD * 4 <= 2 * ARRAY, "merge area");
-  // two arrays, so that the wait before reading one slot covers only its loads
-  __shared__ __attribute__((aligned(16))) uint8_t l0[ARRAY];
-  __shared__ __attribute__((aligned(16))) uint8_t l1[ARRAY];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * ARRAY];
   __shared__ float ml[kWaves * MAXG * 2];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int G = a.group;
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int unit = xcd_unit(blockIdx.x, gridDim.x);
   const int split = unit / a.nkv, kh = unit - split * a.nkv;
   const DecRow r = dec_row(a, m, last_at_or_below(m + DEC_SPLIT0 * a.n, a.n, split));
@@ -105,12 +104,14 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
 #pragma unroll
   for (int ob = 0; ob < NOB; ++ob) oacc[ob] = zero;
   float mrun = kNoScore, lsum = 0.f;
-  // this head's scores of the request: runs of 16, one per page
+  f32x4_t s_page = zero;  // the scores of the page worked on last
+  // this head's scores of the request: runs of 16, page by page the G heads'
+  // (a wavefront stores whole lines)
   float *sc_out = nullptr;
   if (a.scores && c < G) {
     const size_t npv = (size_t)((r.nkeys - r.first + kPageSize - 1) / kPageSize);
-    const size_t run = (size_t)m[DEC_SCORE0 * a.n + r.d] + (size_t)(kh * G + c) * npv;
-    sc_out = a.scores + run * kPageSize + 4 * g - r.first;  // + key of the page's first slot
+    const size_t run = (size_t)m[DEC_SCORE0 * a.n + r.d] + (size_t)kh * G * npv + c;
+    sc_out = a.scores + run * kPageSize + 4 * g;
   }
 
   uint32_t goff[Tr::NDMA];
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
       for (int j = 0; j < 4; ++j)
         if (kp + 4 * g + j >= k1 || kp + 4 * g + j < lo) s[j] = kNoScore;
     }
-    if (sc_out) st_u32x4(sc_out + kp, __builtin_bit_cast(u32x4_t, f32x4_t{s[0], s[1], s[2], s[3]}));
+    s_page = f32x4_t{s[0], s[1], s[2], s[3]};
     float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     mx = fmaxf(mx, shfl_xor_f32(mx, 16));
     mx = fmaxf(mx, shfl_xor_f32(mx, 32));
@@ -202,33 +203,69 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
     }
   };
   // pages pg0 + wave, + 4, ..; lane l of vbt holds the physical page of page
-  // pg0 + l (a split has at most 32)
+  // pg0 + l (a split has at most 64)
   const int npg = pg1 - pg0;
   const int vbt = lane < npg ? bt[pg0 + lane] : -1;
-  auto dma = [&](uint8_t *slot, int i) {
+  const uint32_t page_bytes = (uint32_t)(a.nkv * Tr::BLK);
+  const uint8_t *const kbase = reinterpret_cast<const uint8_t *>(a.kv.k) + (size_t)kh * Tr::BLK;
+  const uint8_t *const vbase = reinterpret_cast<const uint8_t *>(a.kv.v) + (size_t)kh * Tr::BLK;
+  // (its slot's last reads have been waited for: their products are issued)
+  auto dma = [&](uint32_t slot, int i) {
     const int phys = i < npg ? __builtin_amdgcn_readlane(vbt, i) : -1;
-    mdec_dma_page<HD, F8>(slot, goff, a.kv, phys, pg0 + i, k1, a.nkv, kh);
+    const int bytes = (unsigned)phys < (unsigned)a.kv.num_pages
+                          ? min(max(k1 - (pg0 + i) * kPageSize, 0), kPageSize) * Tr::ROW
+                          : 0;  // nothing, zeros in LDS
+    const uint64_t at = (uint64_t)(uint32_t)phys * page_bytes;
+    const u32x4_t rk = range_words(kbase + at, bytes), rv = range_words(vbase + at, bytes);
+#pragma unroll
+    for (int n = 0; n < Tr::NDMA; ++n) {
+      lds_fill16<true>(rk, slot + n * 1024, goff[n]);
+      lds_fill16<true>(rv, slot + Tr::BLK + n * 1024, goff[n]);
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
-  uint8_t *w0 = l0 + wave * Tr::SLOT, *w1 = l1 + wave * Tr::SLOT;
+  const uint8_t *const w0 = lds + 2 * wave * Tr::SLOT, *const w1 = w0 + Tr::SLOT;
+  const uint32_t f0 = lds_at(w0), f1 = f0 + Tr::SLOT;
   constexpr int PAGE_LOADS = 2 * Tr::NDMA;
-  dma(w0, wave);
+  auto keep_scores = [&](int p) {
+    if (sc_out)
+      st_u32x4(sc_out + (size_t)(p * kPageSize - r.first) * G, __builtin_bit_cast(u32x4_t, s_page));
+  };
+  // Operations count down in the order they were issued, stores among them: a
+  // page's scores are stored behind the loads of the next page for its slot, so
+  // that the wait for the other slot leaves them (and the store before them)
+  // outstanding.
+  const bool stores = a.scores != nullptr;
+  dma(f0, wave);
+  dma(f1, wave + kWaves);
   for (int i = wave; i < npg; i += 2 * kWaves) {
-    dma(w1, i + kWaves);
-    wait_loads<PAGE_LOADS>();  // all but w1's: w0 has landed
+    if (stores && i > wave)
+      wait_loads<PAGE_LOADS + 2>();  // w0's loads are older than a store, w1's loads and a store
+    else
+      wait_loads<PAGE_LOADS>();
     update(w0, pg0 + i);
     __builtin_amdgcn_sched_barrier(0);
-    dma(w0, i + 2 * kWaves);
-    wait_loads<PAGE_LOADS>();
-    if (i + kWaves < npg) update(w1, pg0 + i + kWaves);
+    dma(f0, i + 2 * kWaves);
+    keep_scores(pg0 + i);
     __builtin_amdgcn_sched_barrier(0);
+    if (i + kWaves < npg) {
+      if (stores && i > wave)
+        wait_loads<PAGE_LOADS + 2>();
+      else
+        wait_loads<PAGE_LOADS>();
+      update(w1, pg0 + i + kWaves);
+      __builtin_amdgcn_sched_barrier(0);
+      dma(f1, i + 3 * kWaves);
+      keep_scores(pg0 + i + kWaves);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
   wait_loads<0>();
   lsum += shfl_xor_f32(lsum, 16);
   lsum += shfl_xor_f32(lsum, 32);
   // across the waves through LDS, reusing the slots: [wave][h][HD]
   __syncthreads();
-  float *mo = reinterpret_cast<float *>(wave < kWaves / 2 ? l0 : l1) + (wave & 1) * MAXG * HD;
+  float *mo = reinterpret_cast<float *>(lds) + wave * MAXG * HD;
   if (c < G) {
 #pragma unroll
     for (int ob = 0; ob < NOB; ++ob) *reinterpret_cast<f32x4_t *>(mo + c * HD + ob * 16 + g * 4) = oacc[ob];
@@ -250,7 +287,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
     for (int w = 0; w < kWaves; ++w) {
       const float mw = ml[(w * MAXG + h) * 2];
       const float f = mw == kNoScore ? 0.f : fast_exp2(mw - mx);
-      const float *src = reinterpret_cast<const float *>(w < kWaves / 2 ? l0 : l1) + (w & 1) * MAXG * HD;
+      const float *src = reinterpret_cast<const float *>(lds) + w * MAXG * HD;
       L += f * ml[(w * MAXG + h) * 2 + 1];
       O += f * src[h * HD + dim];
     }
@@ -273,7 +310,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
 // weights[t] += sum over the G heads of 2^(s - lse): one block per 1024 keys of
 // a (request, kv head), four keys per thread.  Reads 4 G bytes per key.
 __global__ __launch_bounds__(256) void k_attend_decode_weights(AttendArgs a) {
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int unit = blockIdx.x;
   const int blk = unit / a.nkv, kh = unit - blk * a.nkv;
   const DecRow r = dec_row(a, m, last_at_or_below(m + DEC_WBLOCK0 * a.n, a.n, blk));
@@ -291,10 +328,12 @@ __global__ __launch_bounds__(256) void k_attend_decode_weights(AttendArgs a) {
   // (pages before the first visible key hold no scores)
   if (key / kPageSize >= lo / kPageSize && lo < r.nkeys) {
     const size_t npv = (size_t)((r.nkeys - r.first + kPageSize - 1) / kPageSize);
-    const float *s = a.scores + ((size_t)m[DEC_SCORE0 * a.n + r.d] + (size_t)kh * a.group * npv) * kPageSize + base;
+    const float *s = a.scores +
+                     ((size_t)m[DEC_SCORE0 * a.n + r.d] + (size_t)a.group * (kh * npv + base / kPageSize)) * kPageSize +
+                     base % kPageSize;
     const float *lse = a.lse + (size_t)r.row * a.nq + kh * a.group;
     for (int h = 0; h < a.group; ++h) {
-      const f32x4_t v = *reinterpret_cast<const f32x4_t *>(s + (size_t)h * npv * kPageSize);
+      const f32x4_t v = *reinterpret_cast<const f32x4_t *>(s + h * kPageSize);
       const float z = lse[h] * kLog2e;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -311,12 +350,11 @@ __global__ __launch_bounds__(256) void k_attend_decode_weights(AttendArgs a) {
   }
 }
 
-// Joins the splits of a decode row, one wavefront per query head:
-// o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.
+// Joins the splits of the decode rows that have several, one wavefront per
+// query head.
 template <int HD>
 __global__ __launch_bounds__(256) void k_attend_decode_combine(AttendArgs a) {
-  const int32_t *m = meta_words(a);
-  const int lane = threadIdx.x & 63;
+  const meta_t m = meta_words(a);
   const int qh = blockIdx.y * 4 + (threadIdx.x >> 6);
   if (qh >= a.nq) return;
   const DecRow r = dec_row(a, m, blockIdx.x);
@@ -325,7 +363,7 @@ __global__ __launch_bounds__(256) void k_attend_decode_combine(AttendArgs a) {
   if (ns < 2) return;
   const bool empty = row_first(a, r.row, r.ctx) >= r.nkeys;
   const size_t base = (size_t)m[DEC_SPLIT0 * a.n + r.d] * a.nq + qh;
-  join_splits<HD>(a, base, ns, (size_t)r.row * a.nq + qh, empty, lane);
+  join_splits<HD>(a, base, ns, (size_t)r.row * a.nq + qh, empty, threadIdx.x & 63);
 }
 
 }  // namespace

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, lh = lane >> 5;
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int blk = blockIdx.x / a.nkv, kh = blockIdx.x - blk * a.nkv;
   const int k = last_at_or_below(m + PRE_WBLOCK0 * a.n, a.n, blk);
   const auto field = [&](int f) { return __builtin_amdgcn_readfirstlane(m[f * a.n + k]); };

@@ -58,7 +58,7 @@ struct Head {
   unsigned span;  // candidates: [s0, s0 + span)
   const int32_t *bt;
 };
-__device__ __forceinline__ Head head_of(const EvictArgs &a, const int32_t *m, int seq, int kh) {
+__device__ __forceinline__ Head head_of(const EvictArgs &a, meta_t m, int seq, int kh) {
   Head h;
   h.seq = seq;
   h.kh = kh;
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void k_evict_select(EvictArgs a) {
   __shared__ uint32_t list[kListMost], lim[2];
   __shared__ BinScratch bs;
   __shared__ int n_list, cnt[RUNS * kWaves];  // heavier and (upper half) equal keys of a run's wavefront
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int seq = blockIdx.x / a.nkv;
   const Head h = head_of(a, m, seq, blockIdx.x - seq * a.nkv);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -317,9 +317,9 @@ template <int RB>  // bytes of a key's K (or V) row
 __global__ __launch_bounds__(256) void k_evict_copy(EvictArgs a) {
   constexpr int LPR = RB / 16;                                      // threads per row
   constexpr int STEPS = kPagesPerGroup * kPageSize * LPR / 256;     // 1 .. 4
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int grp = blockIdx.x / a.nkv, kh = blockIdx.x - grp * a.nkv;
-  const int32_t *first = m + EV_GROUP0 * a.S;
+  const meta_t first = m + EV_GROUP0 * a.S;
   const int seq = last_at_or_below(first, a.S, grp);
   const int k = min(m[EV_LEN * a.S + seq], m[EV_KEEP * a.S + seq]);
   const int j0 = (grp - first[seq]) * kPagesPerGroup * kPageSize;
@@ -421,7 +421,7 @@ template <int RB>
 __global__ __launch_bounds__(256) void k_evict_few(EvictArgs a) {
   constexpr int NJ = kEvictFew / 64;
   __shared__ int at[kEvictFew];
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int seq = blockIdx.x / a.nkv;
   const Head h = head_of(a, m, seq, blockIdx.x - seq * a.nkv);
   const int k = min(h.c, h.keep), lane = threadIdx.x & 63;
@@ -476,10 +476,10 @@ struct Segment {
   int seg, at;   // segment of the request, its place in the per-segment arrays
   int t0, t1;    // keys
 };
-__device__ __forceinline__ Segment segment_of(const EvictArgs &a, const int32_t *m, int block) {
+__device__ __forceinline__ Segment segment_of(const EvictArgs &a, meta_t m, int block) {
   Segment s;
   const int g = block / a.nkv, kh = block - g * a.nkv;
-  const int32_t *first = m + EV_SEG0 * a.S;
+  const meta_t first = m + EV_SEG0 * a.S;
   const int seq = last_at_or_below(first, a.S, g);
   s.h = head_of(a, m, seq, kh);
   s.head = seq * a.nkv + kh;
@@ -490,7 +490,7 @@ __device__ __forceinline__ Segment segment_of(const EvictArgs &a, const int32_t 
   s.t1 = min(s.h.c, s.t0 + len);
   return s;
 }
-__device__ __forceinline__ int64_t list_at(const EvictArgs &a, const int32_t *m, const Head &h) {
+__device__ __forceinline__ int64_t list_at(const EvictArgs &a, meta_t m, const Head &h) {
   return ((int64_t)m[EV_LIST0 * a.S + h.seq] * a.nkv + (int64_t)h.kh * ((h.c + 15) / 16)) * 16;
 }
 constexpr int kTopShift = 21;  // the first 11 bits
@@ -546,7 +546,7 @@ __global__ __launch_bounds__(kThreads) void k_evict_list(EvictArgs a) {
   __shared__ uint32_t lv[2 * kRun];
   __shared__ int lt[2 * kRun];
   __shared__ int n_here, base, total;
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const Segment s = segment_of(a, m, blockIdx.x);
   const Head &h = s.h;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -597,7 +597,7 @@ __global__ __launch_bounds__(kThreads) void k_evict_solve(EvictArgs a) {
   __shared__ BinScratch bs;
   __shared__ int hist[kBins];
   __shared__ int seg_g[kEvictSegments], seg_e[kEvictSegments], part_g[kWaves], part_e[kWaves];
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int seq = blockIdx.x / a.nkv;
   const Head h = head_of(a, m, seq, blockIdx.x - seq * a.nkv);
   const int head = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -685,7 +685,7 @@ __global__ __launch_bounds__(kThreads) void k_evict_solve(EvictArgs a) {
 template <int RB>
 __global__ __launch_bounds__(kThreads) void k_evict_place(EvictArgs a) {
   __shared__ int cnt[2 * kWaves], at[2 * kRun];
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const Segment s = segment_of(a, m, blockIdx.x);
   const Head &h = s.h;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;

@@ -37,13 +37,13 @@ struct RotArgs {
 static_assert(sizeof(RotArgs) < 4096, "kernel arguments");
 
 // Request and cache slot of row r.
-__device__ __forceinline__ void row_place(const RotArgs &a, const int32_t *m, int r, int &seq, int &slot) {
+__device__ __forceinline__ void row_place(const RotArgs &a, meta_t m, int r, int &seq, int &slot) {
   if (a.uniform_n > 0) {
     seq = r / a.uniform_n;
     slot = m[seq] + r - seq * a.uniform_n;
     return;
   }
-  const int32_t *first = m + a.S;
+  const meta_t first = m + a.S;
   int lo = 0, hi = a.S - 1;
   while (lo < hi) {  // last request whose first row is <= r
     const int mid = (lo + hi + 1) >> 1;
@@ -67,7 +67,7 @@ template <int HD, bool F8, bool QKN, bool INTER, int NI>
 __global__ __launch_bounds__(256) void k_rotary_append(RotArgs a) {
   constexpr int TPH = HD / 16;
   __shared__ float cs[kMaxRows * HD / 2], sn[kMaxRows * HD / 2];
-  const int32_t *m = meta_words(a);
+  const meta_t m = meta_words(a);
   const int nh = a.nq + 2 * a.nkv, U = nh * TPH, cols = nh * HD;
   const int r0 = blockIdx.x * a.rows_per_block;
   const int nrows = min(a.rows_per_block, a.T - r0);

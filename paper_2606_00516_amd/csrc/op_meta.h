@@ -23,22 +23,26 @@ struct Words {
 // Enqueue the write of n words to dev (device memory).
 hipError_t put_words(const int32_t *words, size_t n, int32_t *dev, hipStream_t st);
 
+// A table as a kernel reads it: read-only while the kernel runs, so entries at
+// uniform places come by scalar loads.
+typedef const __attribute__((address_space(4))) int32_t *meta_t;
+
 // The tables of a kernel whose only parameter is a struct A with members
 // `const int32_t *meta` (null: the words follow in the arguments) and
 // `Words inl`.
 template <class A>
-__device__ __forceinline__ const int32_t *meta_words(const A &a) {
+__device__ __forceinline__ meta_t meta_words(const A &a) {
   typedef const __attribute__((address_space(4))) char *karg_t;
   // the struct is the kernel's first and only parameter: offset 0
   const karg_t p = (karg_t)__builtin_amdgcn_kernarg_segment_ptr();
-  const int32_t *in = (const int32_t *)(p + offsetof(A, inl));
-  return a.meta ? a.meta : in;
+  const meta_t in = (meta_t)(p + offsetof(A, inl));
+  return a.meta ? (meta_t)a.meta : in;
 }
 
 // Index of the last entry of the ascending array first[0 .. n) that is <= v
 // (first[0] <= v); called by whole wavefronts with a uniform v.  Each round
 // probes 64 evenly spaced entries, one per lane.
-__device__ __forceinline__ int last_at_or_below(const int32_t *first, int n, int v) {
+__device__ __forceinline__ int last_at_or_below(meta_t first, int n, int v) {
   const int lane = threadIdx.x & 63;
   int lo = 0;
   while (n > 1) {

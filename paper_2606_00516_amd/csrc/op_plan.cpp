@@ -32,6 +32,12 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   p.n_dec = (int32_t)ones.size();
   p.dec.assign((size_t)DEC_FIELDS * p.n_dec, 0);
   int64_t runs = 0;
+  // the longest splits first: the launch ends on the shortest
+  const auto split_of = [&](int i) {
+    const int32_t c = b.context_lens_host[i];
+    return attend_split_keys(c + 1 - attend_first(c, window));
+  };
+  std::stable_sort(ones.begin(), ones.end(), [&](int32_t x, int32_t y) { return split_of(x) > split_of(y); });
   for (int32_t d = 0; d < p.n_dec; ++d) {
     const int i = ones[d];
     const int32_t c = b.context_lens_host[i], keys = c + 1 - attend_first(c, window);

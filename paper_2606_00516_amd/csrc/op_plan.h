@@ -14,19 +14,26 @@ constexpr int kAttendRows = 128;   // query rows (positions x heads of the group
 constexpr int kWeightKeys = 64;    // keys per block of the weights pass of a chunk
 constexpr int kWeightSpan = 1024;  // keys per block of the weights pass of a decode row
 
-// Keys per split of a decode row that sees `keys` of them, a multiple of the
-// page.  It follows from the request alone, so that its result does not
-// depend on the batch.
+// Keys per split of a decode row that sees `keys` of them: equal shares, a
+// multiple of 64 (a page for each of a block's wavefronts), of at most the
+// size below.  They follow from the request alone, so that its result does
+// not depend on the batch.  Few keys are split finely, for a row alone (1500
+// keys, splits of 128: 6.2 us and 5.1 to join them; of 256: 7.6 and 4.6, of
+// 512: 10.4 and 4.1), the larger splits of many keys cost less to start and
+// join (64 rows over 2350 keys: splits of 256 up to 16384 keys 122 us, of 512
+// 115 us; 13 rows over 69000: of 512 351 us and 35, of 1024 333 and 13).
 __host__ __device__ inline int32_t attend_split_keys(int32_t keys) {
-  return keys <= 1024 ? 128 : keys <= 4096 ? 256 : 512;
+  const int32_t most = keys <= 512 ? 64 : keys <= 2048 ? 128 : keys <= 32768 ? 512 : 1024;
+  const int32_t n = (keys + most - 1) / most;
+  return ((keys + n - 1) / n + 63) & ~63;
 }
 // First key (of a whole page) that the row at position p may see.
 __host__ __device__ inline int32_t attend_first(int32_t p, int32_t window) {
   return window > 0 && p >= window ? (p - window + 1) & ~15 : 0;
 }
 
-// Tables of one attention call.  Decode part: requests with one new row, in
-// batch order; chunk part: the others, the most keys first.  Each table is a
+// Tables of one attention call.  Decode part: requests with one new row, the
+// longest splits first; chunk part: the others, the most keys first.  Each table is a
 // run of arrays (below) of n entries.
 struct AttendPlan {
   int32_t T = 0;
