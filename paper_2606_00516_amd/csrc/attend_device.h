@@ -117,35 +117,40 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 // Joins ns partials (entries base, base + nq, ..) into row entry `at` of out
 // and lse, by one wavefront: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s.
-// Lane s % 64 holds partial s's factor, HD / 64 output dims per lane; up to 16
-// partials' loads are issued together.
+// Lane s % 64 holds partial s's factor, HD / 64 output dims per lane.  Up to 16
+// partials' loads are issued together, the first 16 before their factors are
+// known, so that few partials take one trip to memory.
 template <int HD>
 EB_DEV void join_splits(const AttendArgs &a, size_t base, int ns, size_t at, bool empty, int lane) {
-  constexpr int DPL = HD / 64;
+  constexpr int DPL = HD / 64, N = 16;
   const size_t stride = (size_t)a.nq;
   const float *po = a.part_o + base * HD + lane * DPL, *pm = a.part_ml + base * 2;
-  float mx = kNoScore;
-  for (int s = lane; s < ns; s += 64) mx = fmaxf(mx, pm[s * stride * 2]);
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  float o[N][DPL];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < DPL; ++i) o[u][i] = po[(size_t)min(s0 + u, ns - 1) * stride * HD + i];
+  };
+  // maximum and sum of partial s
+  auto ml = [&](int s) {
+    return s < ns ? *reinterpret_cast<const f32x2_t *>(pm + s * stride * 2) : f32x2_t{kNoScore, 0.f};
+  };
+  f32x2_t v = ml(lane);
+  load(0);
+  float mx = v[0];
+  for (int s = lane + 64; s < ns; s += 64) mx = fmaxf(mx, ml(s)[0]);
   mx = wave_max(mx);
   float den = 0.f, acc[DPL];
 #pragma unroll
   for (int i = 0; i < DPL; ++i) acc[i] = 0.f;
   for (int c = 0; c < ns; c += 64) {
-    const int s = c + lane;
-    float f = 0.f;
-    if (s < ns) {
-      const float ms = pm[s * stride * 2];
-      f = ms == kNoScore ? 0.f : fast_exp2(ms - mx);
-      if (f != 0.f) den += f * pm[s * stride * 2 + 1];
-    }
-    const int n = min(64, ns - c);
-    auto add = [&](int j, auto count) {
-      constexpr int N = decltype(count)::value;
-      float o[N][DPL];
-#pragma unroll
-      for (int u = 0; u < N; ++u)
-#pragma unroll
-        for (int i = 0; i < DPL; ++i) o[u][i] = po[(size_t)min(c + j + u, ns - 1) * stride * HD + i];
+    if (c > 0) v = ml(c + lane);
+    const float f = v[0] == kNoScore ? 0.f : fast_exp2(v[0] - mx);
+    if (f != 0.f) den += f * v[1];
+    for (int j = 0; j < min(64, ns - c); j += N) {
+      if (c + j > 0) load(c + j);
 #pragma unroll
       for (int u = 0; u < N; ++u) {
         // (past the last split the factor is 0; a split that saw nothing wrote no outputs)
@@ -153,10 +158,7 @@ EB_DEV void join_splits(const AttendArgs &a, size_t base, int ns, size_t at, boo
 #pragma unroll
         for (int i = 0; i < DPL; ++i) acc[i] = w != 0.f ? fmaf(w, o[u][i], acc[i]) : acc[i];
       }
-    };
-    int j = 0;
-    for (; j + 8 < n; j += 16) add(j, std::integral_constant<int, 16>{});
-    if (j < n) add(j, std::integral_constant<int, 8>{});
+    }
   }
   den = wave_sum(den);
 #pragma unroll
