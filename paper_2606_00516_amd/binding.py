@@ -547,6 +547,8 @@ def _lens(a, name: str) -> np.ndarray:
         return a
     if a.ndim != 1 or (a.size and not np.issubdtype(a.dtype, np.integer)):
         raise TypeError(f"{name} must be a 1-D array of integers")
+    if a.size and not (-2 ** 31 <= int(a.min()) and int(a.max()) < 2 ** 31):
+        raise ValueError(f"{name} does not fit 32 bits")
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
@@ -606,7 +608,7 @@ def score_mod(scale: float = 0.0, softcap: float = 0.0, slopes: Optional[torch.T
 def _check_mod(h: Handle, batch: HostBatch, m: Optional[ScoreMod]):
     if m is None:
         return None
-    slopes, first, pre = m.held
+    slopes, first, pre = getattr(m, "held", (None, None, None))   # (a struct filled by hand names its own addresses)
     if slopes is not None and slopes.numel() != h.n_q_heads:
         raise ValueError("slopes needs one value per query head")
     if first is not None and first.numel() != batch.c.num_tokens:

@@ -63,6 +63,14 @@ eb_status check_cache(const eb_kv_cache *kv, const char *what) {
   return s;
 }
 
+// Host copy of a cache's block tables, for debug validation.
+eb_status table_copy(const eb_kv_cache *kv, int32_t S, hipStream_t st, std::vector<int32_t> &bt) {
+  bt.resize((size_t)S * kv->max_pages_per_seq);
+  hipError_t e = hipMemcpyAsync(bt.data(), kv->block_tables, bt.size() * 4, hipMemcpyDeviceToHost, st);
+  if (e == hipSuccess) e = hipStreamSynchronize(st);
+  return e == hipSuccess ? EB_OK : api_hip_fail(e, "debug validation copy");
+}
+
 // ---------------------------------------------------------------- rotary
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
@@ -227,9 +235,10 @@ size_t eb_op_attention_mod_workspace_bytes(const eb_handle *h, const eb_batch *b
   return guarded_bytes([&]() -> size_t {
     if (!h || api_check_batch(h, batch, -1) != EB_OK || check_mod(mod, batch) != EB_OK) return 0;
     AttendPlan p;
-    plan_attend(*api_view(h).cfg, *batch, mod ? mod->window : 0, mod ? mod->prefix_lens_host : nullptr,
-                want_weights != 0, 0, p);
-    return p.total;
+    return plan_attend(*api_view(h).cfg, *batch, mod ? mod->window : 0, mod ? mod->prefix_lens_host : nullptr,
+                       want_weights != 0, 0, p)
+               ? p.total
+               : 0;
   });
 }
 
@@ -254,8 +263,9 @@ eb_status eb_op_attention_mod(eb_handle *h, const void *qkv, const eb_kv_cache *
     if (s == EB_OK && mod) s = check_aligned(mod->first_key, "first_key", 4);
     if (s != EB_OK) return s;
     AttendPlan p;
-    plan_attend(*v.cfg, *batch, mod ? mod->window : 0, mod ? mod->prefix_lens_host : nullptr, kv_weights != nullptr,
-                weight_rows, p);
+    if (!plan_attend(*v.cfg, *batch, mod ? mod->window : 0, mod ? mod->prefix_lens_host : nullptr,
+                     kv_weights != nullptr, weight_rows, p))
+      return api_fail(EB_ERR_LIMITS, "more keys than a launch holds");
     s = api_check_ws(ws, ws_bytes, p.total);
     if (s == EB_OK) s = check_device(v);
     if (s != EB_OK) return s;
@@ -277,6 +287,8 @@ eb_status eb_op_attention_mod(eb_handle *h, const void *qkv, const eb_kv_cache *
       c.first_key = mod->first_key;
       c.window = mod->window;
     }
+    const double unit = 2.0 * c.scale * c.kv.ks / (c.softcap > 0.f ? c.softcap : 1.0);
+    if (!(unit < 1e38)) return api_fail(EB_ERR_CONFIG, "scale (with the cache's scale, over softcap) leaves fp32");
     c.plan = &p;
     c.ws = static_cast<char *>(ws);
     const hipError_t e = launch_attend(*v.shape, c, st);
@@ -339,10 +351,8 @@ eb_status eb_op_kv_evict(eb_handle *h, const eb_kv_cache *src, const float *kv_w
       std::vector<char> seen((size_t)dst->num_pages, 0);
       for (int d = 0; d < 2; ++d) {
         const eb_kv_cache *kv = d ? dst : src;
-        bt[d].resize((size_t)num_seqs * kv->max_pages_per_seq);
-        hipError_t e = hipMemcpyAsync(bt[d].data(), kv->block_tables, bt[d].size() * 4, hipMemcpyDeviceToHost, st);
-        if (e == hipSuccess) e = hipStreamSynchronize(st);
-        if (e != hipSuccess) return api_hip_fail(e, "debug validation copy");
+        s = table_copy(kv, num_seqs, st, bt[d]);
+        if (s != EB_OK) return s;
         for (int i = 0; i < num_seqs; ++i) {
           const int32_t len = d ? std::min(lens_host[i], keep_lens_host[i]) : lens_host[i];
           for (int64_t j = 0; j < ((int64_t)len + kPageSize - 1) / kPageSize; ++j) {

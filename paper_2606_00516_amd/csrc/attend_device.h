@@ -27,7 +27,7 @@ struct AttendArgs {
   float qscale;                                    // no cap: to log2 units; cap: 2 log2(e) scale / cap
   float cap2;                                      // cap in log2 units
   // cap tanh(scale raw / cap) log2(e) = raw (tanh_c[0] + tanh_c[1] raw^2 + ..)
-  // up to |raw| = small_raw (0: the polynomial's coefficients leave fp32)
+  // up to |raw| = small_raw (-1: the polynomial's coefficients leave fp32)
   float small_raw, tanh_c[5];
   const int32_t *meta;
   Words inl;

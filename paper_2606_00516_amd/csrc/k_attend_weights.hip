@@ -301,7 +301,7 @@ hipError_t launch_attend(const Shape &s, const AttendCall &c, hipStream_t st) {
       a.tanh_c[i] = (float)(f * k[i]);
       ok = ok && std::fabs(a.tanh_c[i]) > 1e-36f && std::fabs(a.tanh_c[i]) < 1e36f;
     }
-    a.small_raw = ok ? (float)(0.7 / y) : 0.f;
+    a.small_raw = ok ? (float)(0.7 / y) : -1.f;  // (below every score: never)
   }
   hipError_t e = hipSuccess;
   if (p.n_dec > 0) {

@@ -23,7 +23,7 @@ int32_t chunk_splits(int32_t rows, int32_t kv_heads, int32_t q_blocks, int32_t t
 }
 }  // namespace
 
-void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
+bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
                  int32_t weight_rows, AttendPlan &p) {
   p = AttendPlan();
   p.T = b.num_tokens;
@@ -37,6 +37,11 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   p.n_dec = (int32_t)ones.size();
   p.dec.assign((size_t)DEC_FIELDS * p.n_dec, 0);
   int64_t runs = 0;
+  int32_t part = 0;  // partials of the chunks, behind those of the decode rows
+  const auto fits = [&]() {  // (each request adds less than 2^30 to a count: looked at after each, none wraps)
+    return std::max({p.dec_splits, p.dec_wblocks, p.pre_tiles, p.pre_wblocks}) <= kMostBlocks / nkv &&
+           part <= 0x3FFFFFFF && runs <= 0x7FFFFFFF;
+  };
   // the longest splits first: the launch ends on the shortest
   const auto split_of = [&](int i) {
     const int32_t c = b.context_lens_host[i];
@@ -61,11 +66,12 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
       p.dec_wblocks += (keys + kWeightSpan - 1) / kWeightSpan;
       runs += (int64_t)((keys + 15) / 16) * cfg.n_q_heads;
     }
+    if (!fits()) return false;
   }
   std::stable_sort(many.begin(), many.end(), [&](int32_t x, int32_t y) { return keys_of(x) > keys_of(y); });
   p.n_pre = (int32_t)many.size();
   p.pre.assign((size_t)PRE_FIELDS * p.n_pre, 0);
-  int32_t part = p.dec_splits;
+  part = p.dec_splits;
   for (int32_t k = 0; k < p.n_pre; ++k) {
     const int i = many[k];
     const int32_t c = b.context_lens_host[i], n = b.chunk_lens_host[i], nqb = (n + bq - 1) / bq;
@@ -102,6 +108,7 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
       const int32_t first = std::min(c, attend_first(c + j0, window)) / kWeightKeys;
       p.pre_wblocks += (c + n + kWeightKeys - 1) / kWeightKeys - first;
     }
+    if (!fits()) return false;
   }
   size_t off = 0;
   const auto take = [&](size_t bytes) {
@@ -116,6 +123,7 @@ void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   p.o_part_ml = take((size_t)part * cfg.n_q_heads * 8);
   p.o_scores = take((size_t)runs * 64);
   p.total = off;
+  return true;
 }
 
 bool plan_evict(int32_t n_kv, int32_t S, const int32_t *lens, const int32_t *keep, EvictPlan &p) {
@@ -136,7 +144,7 @@ bool plan_evict(int32_t n_kv, int32_t S, const int32_t *lens, const int32_t *kee
     runs += (c + 15) / 16;
     p.max_len = std::max(p.max_len, c);
     p.max_keep = std::max(p.max_keep, k);
-    if (p.groups * n_kv > 0x7FFFFFFF || p.segments * n_kv > 0x7FFFFFFF || runs > 0x7FFFFFFF) return false;
+    if (std::max(p.groups, p.segments) > kMostBlocks / n_kv || runs > 0x7FFFFFFF) return false;
   }
   size_t off = 0;
   const auto take = [&](size_t bytes) {

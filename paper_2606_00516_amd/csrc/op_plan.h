@@ -58,9 +58,12 @@ enum PreField {
 };
 
 // window 0: none; prefix: per request, or null.  The batch has passed
-// check_batch.
-void plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
+// check_batch.  False: more blocks or table entries than a launch holds.
+bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
                  int32_t weight_rows, AttendPlan &p);
+
+// Blocks of a launch: their threads (up to 512 each) are counted in 32 bits.
+constexpr int64_t kMostBlocks = 0x7FFFFF;
 
 // ---- eviction ----
 constexpr int kEvictFew = 512;         // keys of the longest request: one wavefront chooses

@@ -1,0 +1,148 @@
+"""The operators on the paged cache where they could go wrong together or at
+their ends: caches past 32-bit offsets, calls at the same time, masks and
+scores combined, scales that leave a polynomial, and what is refused."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_00516_amd import binding as B
+from tests import _cache_ops as R
+from tests.test_gpu_cache_attention import _qkv, check, run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_pages_past_32_bit_offsets(fp8):
+    # 16384 elements a page: more than 2^31 elements, 2^32 bytes in bf16, before the pages in use
+    sh, far = R.shape(8, 8, 128), 140000
+    ctx, chk = np.array([700, 90, 0]), np.array([1, 40, 130])
+    n, T = ctx + chk, int(chk.sum())
+    small = R.make_cache(n, 8, 128, fp8, 3, spare=60, poison=False)
+    pages, used = small.k.shape[0], small.bt.max().item() + 1
+    free = torch.tensor(sorted(set(range(pages)) - set(small.bt[small.bt >= 0].tolist())), dtype=torch.int32)
+    assert used <= pages and len(free) == 60
+    to = torch.stack([free[20 * i:20 * i + 20] for i in range(3)])   # the destination's pages
+    h, batch, qkv = B.Handle(sh, 3, T), B.HostBatch(ctx, chk), _qkv(T, sh, 5)
+    w0 = torch.rand(small.k.shape[:3], generator=torch.Generator().manual_seed(1))
+    res = []
+    for base in (0, far):
+        k = torch.empty((base + pages, *small.k.shape[1:]), dtype=small.k.dtype, device="cuda")
+        v, w = torch.empty_like(k), torch.empty(k.shape[:3], device="cuda")
+        k[base:], v[base:], w[base:] = small.k.cuda(), small.v.cuda(), w0.cuda()
+        bt = torch.where(small.bt >= 0, small.bt + base, small.bt).cuda()
+        kv, x = B.kv_struct(k, v, bt, small.scales), qkv.cuda()
+        dst = B.kv_struct(k, v, (to + base).cuda(), small.scales)
+        lse = torch.empty(T, 8, device="cuda")
+        B.eb_op_rotary_kv_append(h, B.rotary(1e4), x, kv, batch)
+        out = B.eb_op_attention_mod(h, x, kv, batch, B.score_mod(softcap=30.0, window=200), lse=lse, kv_weights=w)
+        kept = torch.zeros(3, 8, 300, dtype=torch.int32, device="cuda")
+        B.eb_op_kv_evict(h, kv, w, n, [300, 100, 60], dst, w, 4, 20, kept)
+        torch.cuda.synchronize()
+        res.append([t.cpu() for t in (x, out, lse, kept, k[base:].view(torch.uint8), v[base:].view(torch.uint8), w[base:])])
+        del k, v, w, kv, dst, bt
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
+def test_two_calls_at_once():
+    sh = R.shape(8, 2, 128)
+    h, T = B.Handle(sh, 4, 300), 211
+    ctx, chk = np.array([3000, 100, 0, 1500]), np.array([1, 80, 129, 1])
+    s = [torch.cuda.Stream() for _ in range(2)]
+    one = []
+    for k in range(2):
+        d = R.make_cache(ctx + chk, 2, 128, seed=k, poison=False).cuda()
+        batch, mod = B.HostBatch(ctx, chk), B.score_mod(softcap=20.0)
+        ws = B.alloc_workspace(B.eb_op_attention_mod_workspace_bytes(h, batch, mod, True))
+        one.append((d, B.kv_struct(d.k, d.v, d.bt), batch, mod, ws, _qkv(T, sh, k).cuda(),
+                    torch.empty(T, 1024, dtype=torch.bfloat16, device="cuda"), torch.zeros(d.k.shape[:3], device="cuda")))
+
+    def go(k, stream=None):
+        d, kv, batch, mod, ws, x, out, w = one[k]
+        B.eb_op_attention_mod(h, x, kv, batch, mod, out, None, w, ws=ws, stream=stream)
+    want = []
+    for k in range(2):
+        one[k][7].zero_()
+        go(k)
+        torch.cuda.synchronize()
+        want.append((one[k][6].clone(), one[k][7].clone()))
+    for _ in range(20):
+        for k in range(2):
+            one[k][6].zero_()
+            one[k][7].zero_()
+        torch.cuda.synchronize()
+        for k in range(2):
+            go(k, s[k])
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert torch.equal(one[k][6], want[k][0]) and torch.equal(one[k][7], want[k][1])
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (16, 2, 128)])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_everything_at_once(heads, fp8):
+    sh = R.shape(*heads)
+    ctx, chk = [400, 37, 0, 129, 1000], [1, 70, 200, 1, 3]
+    rng = np.random.default_rng(4)
+    first = np.concatenate([rng.integers(0, c + 1 + np.arange(n)) for c, n in zip(ctx, chk)])
+    first[[5, 90]] = 2 ** 31 - 1          # rows that see nothing, but for a prefix
+    first[[7, 120]] = -2 ** 31            # no bound
+    slopes = [2.0 ** (-8.0 * (i + 1) / sh.n_q_heads) for i in range(sh.n_q_heads)]
+    got, ref, _, _ = run(sh, ctx, chk, fp8=fp8, window=90, prefix=[0, 60, 150, 130, 1003], first=first, softcap=30.0,
+                         slopes=slopes, scale=0.2, weights=True, weight_rows=50)
+    check(got, ref)
+
+
+@pytest.mark.parametrize("chk", [1, 40])
+def test_zero_products_under_a_steep_cap(chk):
+    # scale / softcap = 1e8: the cap's polynomial has no fp32 coefficients; tanh(0) is 0 all the same
+    sh = R.shape(4, 2, 64)
+    qkv = _qkv(chk, sh, 1)
+    qkv[:, :256] = 0
+    got, ref, _, _ = run(sh, [30], [chk], qkv=qkv, scale=1e5, softcap=1e-3, weights=True)
+    check(got, ref)
+
+
+def test_what_leaves_the_range_is_refused():
+    h = B.Handle(R.shape(8, 2, 64), 4, 64)
+    kv = B.KvCache(0x10000, 0x10000, 4, 0x10000, 2 ** 27, 0, 1.0, 1.0)
+    L, long = B.lib(), B.HostBatch([2 ** 30 - 100], [4])
+
+    def call(mod, b, w=None):
+        return L.eb_op_attention_mod(h.h, 0x10000, kv, b.c, mod, 0x10000, None, w, 0, 0x10000, 1 << 62, None)
+    assert call(None, long, 0x10000) == -7                  # blocks of the weights pass
+    assert B.eb_op_attention_mod_workspace_bytes(h, long, None, True) == 0
+    assert B.eb_op_attention_mod_workspace_bytes(h, long, B.score_mod(window=1000), True) > 0
+    assert call(B.score_mod(scale=1e30, softcap=1e-9), B.HostBatch([3], [1])) == -2
+    assert B.eb_op_kv_evict_workspace_bytes(h, [2 ** 30 - 1], [2 ** 30 - 1]) == 0
+    with pytest.raises(ValueError):
+        B.eb_op_kv_evict_workspace_bytes(h, [2 ** 32 + 5], [5])
+
+
+def test_debug_validation(monkeypatch):
+    monkeypatch.setenv("EB_DEBUG_VALIDATE", "1")
+    sh = R.shape(4, 2, 64)
+    h = B.Handle(sh, 2, 8)
+    monkeypatch.delenv("EB_DEBUG_VALIDATE")
+    d = R.make_cache([40, 40], 2, 64, seed=1, poison=False).cuda()
+    shared = d.bt.clone()
+    shared[1, 0] = shared[0, 0]
+    w, x = torch.zeros(d.k.shape[:3], device="cuda"), _qkv(2, sh, 2).cuda()
+    batch = B.HostBatch([39, 39], [1, 1])
+    B.eb_op_attention_mod(h, x, B.kv_struct(d.k, d.v, d.bt), batch, kv_weights=w)
+    with pytest.raises(B.EbError, match="twice"):
+        B.eb_op_attention_mod(h, x, B.kv_struct(d.k, d.v, shared), batch, kv_weights=w)
+    with pytest.raises(B.EbError, match="in use"):
+        B.eb_op_kv_evict(h, B.kv_struct(d.k, d.v, d.bt), w, [40, 40], [16, 16], B.kv_struct(d.k, d.v, d.bt))
+    torch.cuda.synchronize()
+
+
+def test_a_struct_filled_by_hand():
+    sh = R.shape(4, 2, 64)
+    h = B.Handle(sh, 1, 8)
+    d = R.make_cache([40], 2, 64, seed=1, poison=False).cuda()
+    kv, x, b = B.kv_struct(d.k, d.v, d.bt), _qkv(1, sh, 2).cuda(), B.HostBatch([39], [1])
+    want = B.eb_op_attention_mod(h, x, kv, b, B.score_mod(softcap=5.0, window=8))
+    assert torch.equal(B.eb_op_attention_mod(h, x, kv, b, B.ScoreMod(softcap=5.0, window=8)), want)
+    assert torch.equal(B.eb_op_attention_mod(h, x, kv, b, B.ScoreMod()), B.eb_op_attention_mod(h, x, kv, b))
