@@ -16,9 +16,12 @@ namespace eb {
 // few dozen words more.
 constexpr int kInlineInts = 768;
 
-struct Words {
-  int32_t w[kInlineInts];
+template <int N>
+struct WordsOf {
+  static constexpr size_t kMost = N;
+  int32_t w[N];
 };
+using Words = WordsOf<kInlineInts>;
 
 // Enqueue the write of n words to dev (device memory).
 hipError_t put_words(const int32_t *words, size_t n, int32_t *dev, hipStream_t st);
@@ -29,7 +32,7 @@ typedef const __attribute__((address_space(4))) int32_t *meta_t;
 
 // The tables of a kernel whose only parameter is a struct A with members
 // `const int32_t *meta` (null: the words follow in the arguments) and
-// `Words inl`.
+// `Words inl` (or another WordsOf).
 template <class A>
 __device__ __forceinline__ meta_t meta_words(const A &a) {
   typedef const __attribute__((address_space(4))) char *karg_t;
