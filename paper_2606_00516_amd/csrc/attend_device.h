@@ -79,10 +79,13 @@ EB_DEV void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
 }
 
-// A buffer range (uniform) as the four words of its descriptor.
+// A buffer range (uniform) as the four words of its descriptor.  SAID: says so
+// to the compiler, where it does not see it (where it does, the saying cost
+// registers: capped chunks 2.99 ms instead of 2.74).
+template <bool SAID = false>
 EB_DEV u32x4_t range_words(const uint8_t *base, int bytes) {
   const uint64_t b = (uint64_t)base;
-  auto u = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+  auto u = [](uint32_t v) { return SAID ? (uint32_t)__builtin_amdgcn_readfirstlane((int)v) : v; };
   return u32x4_t{u((uint32_t)b), u((uint32_t)(b >> 32) & 0xFFFFu), u((uint32_t)bytes), 0x00020000u};
 }
 // One 16-byte-per-lane load from a buffer range (uniform) straight into LDS:

@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
                           ? min(max(k1 - (pg0 + i) * kPageSize, 0), kPageSize) * Tr::ROW
                           : 0;  // nothing, zeros in LDS
     const uint64_t at = (uint64_t)(uint32_t)phys * page_bytes;
-    const u32x4_t rk = range_words(kbase + at, bytes), rv = range_words(vbase + at, bytes);
+    const u32x4_t rk = range_words<true>(kbase + at, bytes), rv = range_words<true>(vbase + at, bytes);
 #pragma unroll
     for (int n = 0; n < Tr::NDMA; ++n) {
       lds_fill16<true>(rk, slot + n * 1024, goff[n]);
