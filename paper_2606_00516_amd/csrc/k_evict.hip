@@ -73,12 +73,12 @@ __device__ __forceinline__ Head head_of(const EvictArgs &a, meta_t m, int seq, i
   return h;
 }
 
-// fp32 in an unsigned order: larger numbers are larger integers, NaN above
-// all, both zeros the same.
-constexpr uint32_t kZeroWeight = 0x80000000u;
+// fp32 in an unsigned order: larger numbers are larger integers, every NaN
+// above all and like the others, both zeros the same.
+constexpr uint32_t kZeroWeight = 0x80000000u, kNanWeight = 0xFFC00000u;
 EB_DEV uint32_t ordered(float f) {
   const uint32_t u = __float_as_uint(f + 0.0f);
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+  return f != f ? kNanWeight : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
 // N runs of four keys per thread from key t0 on, run j from t0 + 2048 j + 4 tid.

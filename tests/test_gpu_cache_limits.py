@@ -7,6 +7,7 @@ import torch
 
 from paper_2606_00516_amd import binding as B
 from tests import _cache_ops as R
+from tests import test_gpu_cache_evict as E
 from tests.test_gpu_cache_attention import _qkv, check, run
 
 pytestmark = pytest.mark.gpu
@@ -146,3 +147,13 @@ def test_a_struct_filled_by_hand():
     want = B.eb_op_attention_mod(h, x, kv, b, B.score_mod(softcap=5.0, window=8))
     assert torch.equal(B.eb_op_attention_mod(h, x, kv, b, B.ScoreMod(softcap=5.0, window=8)), want)
     assert torch.equal(B.eb_op_attention_mod(h, x, kv, b, B.ScoreMod()), B.eb_op_attention_mod(h, x, kv, b))
+
+
+@pytest.mark.parametrize("lens", [[300, 90], [5000, 700], [20000, 300]])
+def test_nan_weights_of_any_sign_are_largest(lens):
+    def make(w, src, g):
+        bits = torch.tensor([0x7FC00000, 0x7FC00001, 0x7F800001, -0x400000, -0x3FFFFF, -1], dtype=torch.int32)
+        u = torch.randint(0, 40, w.shape, generator=g)
+        return torch.where(u < 6, bits[u.clamp(max=5)].view(torch.float32), w)
+    E.run(R.shape(4, 2, 64), lens, [n // 10 for n in lens], 1, 2, make=make)
+    E.run(R.shape(4, 2, 64), lens, [n // 3 for n in lens], 1, 2, make=make)
