@@ -24,6 +24,7 @@ struct AttendArgs {
   const float *slopes;
   KV kv;
   int32_t nq, nkv, group, window, n, weight_rows;  // n: requests of the table
+  int32_t stash;                                   // bytes of LDS for a decode split's scores; 0: stored as they come
   float qscale;                                    // no cap: to log2 units; cap: 2 log2(e) scale / cap
   float cap2;                                      // cap in log2 units
   // cap tanh(scale raw / cap) log2(e) = raw (tanh_c[0] + tanh_c[1] raw^2 + ..)

@@ -6,7 +6,7 @@
 // HBM.  Its four wavefronts stream the split's pages w, w + 4, .. through
 // two LDS slots each (direct loads, no registers) with one page in flight
 // while another is worked on; at two blocks per CU that is 64 KiB in flight
-// per CU (64 rows over 2350 keys on average, 8 kv heads, bf16: 110 us, 5.6 TB/s;
+// per CU (64 rows over 2350 keys on average, 8 kv heads, bf16: 109 us, 5.6 TB/s;
 // 13 rows over 69000, 8 bits: 327 us, 5.6 TB/s).  Scores are formed as S^T = K Q^T on 16x16x32 products (16 tokens x
 // 16 columns, G of them heads; lane l holds tokens 4 (l / 16) .. + 3 of head
 // l % 16), so the cap, the bias and the mask cost 4 values per lane and page
@@ -15,7 +15,7 @@
 // matrix, which is exact.
 //
 // Splits are joined by k_attend_decode_combine; with weights, the scores are left
-// in the workspace (4 G bytes per key beside the 4 hd read: 110 -> 126 us) and
+// in the workspace (4 G bytes per key beside the 4 hd read: 112 -> 125 us) and
 // k_attend_decode_weights turns them into normalised weights once the rows'
 // log-sum-exp is known (9 us), instead of reading K a second time.
 #include "attend_device.h"
@@ -54,9 +54,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
   using Tr = MdecTraits<HD, F8>;
   constexpr int NKS = HD / 32, NOB = HD / 16, MAXG = 8;
   constexpr int ARRAY = kWaves * Tr::SLOT;
-  static_assert(kWaves * MAXG * HD * 4 <= 2 * ARRAY, "merge area");
+  static_assert(kWaves * MAXG * (HD + 2) * 4 <= 2 * ARRAY, "merge area");
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * ARRAY];
-  __shared__ float ml[kWaves * MAXG * 2];
+  extern __shared__ __attribute__((aligned(16))) float stash[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
@@ -105,15 +105,6 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
   for (int ob = 0; ob < NOB; ++ob) oacc[ob] = zero;
   float mrun = kNoScore, lsum = 0.f;
   f32x4_t s_page = zero;  // the scores of the page worked on last
-  // this head's scores of the request: runs of 16, page by page the G heads'
-  // (a wavefront stores whole lines)
-  float *sc_out = nullptr;
-  if (a.scores && c < G) {
-    const size_t npv = (size_t)((r.nkeys - r.first + kPageSize - 1) / kPageSize);
-    const size_t run = (size_t)m[DEC_SCORE0 * a.n + r.d] + (size_t)kh * G * npv + c;
-    sc_out = a.scores + run * kPageSize + 4 * g;
-  }
-
   uint32_t goff[Tr::NDMA];
 #pragma unroll
   for (int i = 0; i < Tr::NDMA; ++i) {
@@ -227,15 +218,29 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
   const uint8_t *const w0 = lds + 2 * wave * Tr::SLOT, *const w1 = w0 + Tr::SLOT;
   const uint32_t f0 = lds_at(w0), f1 = f0 + Tr::SLOT;
   constexpr int PAGE_LOADS = 2 * Tr::NDMA;
+  // The scores of the request: runs of 16, page by page the G heads' (a
+  // wavefront stores whole lines).  They wait in LDS for the end of the split:
+  // loads and stores count down together in the order they were issued, and
+  // waiting for a page's loads behind a store took longer (64 rows over 2350
+  // keys, the whole call: 140 us, 138 so; 8 bits 84 and 82; what is left, 11
+  // us, is the writing of 19 MB itself).  Where the LDS is short they are stored
+  // behind the loads of the next page for their slot, so that the wait for the
+  // other slot leaves them (and the store before them) outstanding.
+  const bool stores = a.scores && !a.stash;
+  float *split_scores = nullptr;
+  if (a.scores) {
+    const size_t npv = (size_t)((r.nkeys - r.first + kPageSize - 1) / kPageSize);
+    split_scores = a.scores + ((size_t)m[DEC_SCORE0 * a.n + r.d] + (size_t)kh * G * npv) * kPageSize +
+                   (size_t)(pg0 * kPageSize - r.first) * G;
+  }
   auto keep_scores = [&](int p) {
-    if (sc_out)
-      st_u32x4(sc_out + (size_t)(p * kPageSize - r.first) * G, __builtin_bit_cast(u32x4_t, s_page));
+    if (!a.scores || c >= G) return;
+    const int to = ((p - pg0) * G + c) * kPageSize + 4 * g;
+    if (a.stash)
+      *reinterpret_cast<f32x4_t *>(stash + to) = s_page;
+    else
+      *reinterpret_cast<f32x4_t *>(split_scores + to) = s_page;
   };
-  // Operations count down in the order they were issued, stores among them: a
-  // page's scores are stored behind the loads of the next page for its slot, so
-  // that the wait for the other slot leaves them (and the store before them)
-  // outstanding.
-  const bool stores = a.scores != nullptr;
   dma(f0, wave);
   dma(f1, wave + kWaves);
   for (int i = wave; i < npg; i += 2 * kWaves) {
@@ -263,9 +268,13 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
   wait_loads<0>();
   lsum += shfl_xor_f32(lsum, 16);
   lsum += shfl_xor_f32(lsum, 32);
-  // across the waves through LDS, reusing the slots: [wave][h][HD]
+  // across the waves through LDS, reusing the slots: [wave][h][HD], then [wave][h][2]
   __syncthreads();
-  float *mo = reinterpret_cast<float *>(lds) + wave * MAXG * HD;
+  if (a.stash)
+    for (int e = 4 * threadIdx.x; e < npg * G * kPageSize; e += 4 * 256)
+      *reinterpret_cast<f32x4_t *>(split_scores + e) = *reinterpret_cast<const f32x4_t *>(stash + e);
+  float *const mo = reinterpret_cast<float *>(lds) + wave * MAXG * HD;
+  float *const ml = reinterpret_cast<float *>(lds) + kWaves * MAXG * HD;
   if (c < G) {
 #pragma unroll
     for (int ob = 0; ob < NOB; ++ob) *reinterpret_cast<f32x4_t *>(mo + c * HD + ob * 16 + g * 4) = oacc[ob];
@@ -374,13 +383,13 @@ hipError_t launch_attend_decode(const Shape &s, const AttendCall &c, const Atten
 #define EB_DEC(HD_, F8_)                                                                                       \
   do {                                                                                                         \
     if (c.softcap > 0.f && c.slopes)                                                                           \
-      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, true, true>), grid, dim3(256), 0, st, a);                  \
+      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, true, true>), grid, dim3(256), a.stash, st, a);            \
     else if (c.softcap > 0.f)                                                                                  \
-      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, true, false>), grid, dim3(256), 0, st, a);                 \
+      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, true, false>), grid, dim3(256), a.stash, st, a);           \
     else if (c.slopes)                                                                                         \
-      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, false, true>), grid, dim3(256), 0, st, a);                 \
+      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, false, true>), grid, dim3(256), a.stash, st, a);           \
     else                                                                                                       \
-      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, false, false>), grid, dim3(256), 0, st, a);                \
+      hipLaunchKernelGGL((k_attend_decode<HD_, F8_, false, false>), grid, dim3(256), a.stash, st, a);          \
   } while (0)
   if (s.hd == 128) {
     if (a.kv.f8)

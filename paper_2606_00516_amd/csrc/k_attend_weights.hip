@@ -306,6 +306,9 @@ hipError_t launch_attend(const Shape &s, const AttendCall &c, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (p.n_dec > 0) {
     e = with_table(a, p.dec, p.n_dec, c.ws + p.o_dec, st);
+    // A split's scores wait in LDS for its end, if two blocks still share a CU.
+    const size_t slots = (size_t)256 * s.hd * (c.kv.f8 ? 1 : 2), stash = (size_t)p.dec_most * a.group * sizeof(float);
+    a.stash = c.weights && slots + stash <= 80 * 1024 ? (int32_t)stash : 0;
     if (e == hipSuccess) e = launch_attend_decode(s, c, a, st);
   }
   if (e == hipSuccess && p.n_pre > 0) {

@@ -61,6 +61,7 @@ bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
     f[DEC_WBLOCK0 * n] = p.dec_wblocks;
     f[DEC_SCORE0 * n] = (int32_t)runs;
     p.dec_splits += ns;
+    p.dec_most = std::max(p.dec_most, per);
     if (ns > 1) p.dec_combine = true;
     if (weights) {
       p.dec_wblocks += (keys + kWeightSpan - 1) / kWeightSpan;

@@ -38,6 +38,7 @@ __host__ __device__ inline int32_t attend_first(int32_t p, int32_t window) {
 struct AttendPlan {
   int32_t T = 0;
   int32_t n_dec = 0, dec_splits = 0, dec_wblocks = 0;
+  int32_t dec_most = 0;  // keys of the longest split
   bool dec_combine = false;
   std::vector<int32_t> dec;
   int32_t n_pre = 0, pre_tiles = 0, pre_comb_rows = 0, pre_wblocks = 0;
