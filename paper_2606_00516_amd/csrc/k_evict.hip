@@ -10,15 +10,20 @@
 // counts, of the heavier and of the equal ones before it, whether it stays and
 // where it goes.  Three forms, by the longest request of the call:
 //  - to 512 keys (k_evict_few): one wavefront per (request, kv head) finds the
-//    threshold bit by bit with ballots, without a barrier, and its block copies.
+//    threshold bit by bit with ballots, without a barrier, and its block copies
+//    (three requests of 250 to 330 keys: 8.9 us; the next form's two launches
+//    16.5).
 //  - to 16384 keys (k_evict_select, k_evict_copy): a block holds a head's
 //    weights in registers and finds the bin of the threshold by a histogram of
 //    the 11 bits from the highest in which the candidates differ, then the
-//    threshold among the bin's few keys.
+//    threshold among the bin's few keys (32 requests of 4350 keys and 8 heads:
+//    12 us, and 109 for the copy of 4000 keys each, 4.9 TB/s).
 //  - longer (k_evict_hist, _list, _solve, _place): the same over segments of
 //    4096 keys, as many blocks as there are segments; the histogram and the
-//    list of the bin's keys are in the workspace.  One block per head took 99
-//    us for four requests of 40000 to 66000 keys and 8 heads, the copy 27.
+//    list of the bin's keys are in the workspace (16000 keys, 8 heads, this form
+//    and the one before: one request 23.9 and 22.9 us, 32 requests 61 and 50;
+//    four requests of 40000 to 66000 keys: 24 us to choose, one block per head
+//    99; the copy 38 with its counting).
 #include <string.h>
 
 #include "device_common.h"

@@ -9,7 +9,8 @@
 // reduced angle, the products are fp32 and each result is rounded once.
 //
 // The work is 3 R operations per head against 4 R + bytes moved: memory bound,
-// and at a few rows bound by one launch's latency.  So every block issues
+// and at a few rows bound by one launch's latency (7000 rows of 48 heads of 128:
+// 32.7 us, 5.2 TB/s; one row 2.9 us).  So every block issues
 // all of its loads, forms the angles of its rows while they are in flight
 // (once per row, shared by all heads through LDS) and then stores.
 #include <string.h>
@@ -242,7 +243,9 @@ hipError_t launch_rotary_append(const Shape &s, const RotaryCall &c, hipStream_t
     if (e != hipSuccess) return e;
   }
   // A wide call takes up to 1024 units (four per thread, 128 bytes in flight
-  // each) of whole rows per block, a narrow one a single unit per thread.
+  // each) of whole rows per block, a narrow one a single unit per thread (rows
+  // of 48 heads of 128, narrow and wide: 256 3.7 and 5.0 us, 1000 10.1 both, 2000
+  // 17.7 and 16.5).
   const int U = (s.nq + 2 * s.nkv) * (s.hd / 16);
   const bool wide = (long)c.T * U >= 1024L * 512;
   const int per = wide ? 1024 : 256;
