@@ -343,6 +343,31 @@ __device__ __forceinline__ void decode_load_q(const uint16_t *__restrict__ qkv, 
 template <int G>
 constexpr bool kDecodeMfma = G >= 4;
 
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+// Start the loads of page p (physical page phys, -1 past the end) K and V
+// blocks into a slot; slots at or past k1 (and pages past the end or with a
+// bad table entry) land as zeros without memory traffic, so cache poison
+// never reaches the products.
+template <int HD, bool F8>
+__device__ __forceinline__ void mdec_dma_page(uint8_t *slot, const uint32_t *goff, const KV kv, int phys, int p,
+                                              int k1, int nkv, int kh) {
+  using Tr = MdecTraits<HD, F8>;
+  const int nvalid = min(max(k1 - p * kPageSize, 0), kPageSize);
+  const bool ok = phys >= 0 && phys < kv.num_pages;
+  const size_t off = ok ? ((size_t)phys * nkv + kh) * kPageSize * HD : 0;
+  // wave-uniform by construction; said so, so the descriptor stays scalar
+  const int bytes = __builtin_amdgcn_readfirstlane(ok ? nvalid * Tr::ROW : 0);
+  const buf_rsrc_t rk = F8 ? make_rsrc(kv.k8() + off, bytes) : make_rsrc(kv.k + off, bytes);
+  const buf_rsrc_t rv = F8 ? make_rsrc(kv.v8() + off, bytes) : make_rsrc(kv.v + off, bytes);
+#pragma unroll
+  for (int i = 0; i < Tr::NDMA; ++i) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void_t *)(slot + i * 1024), 16, goff[i], 0, 0, kAuxNT);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void_t *)(slot + Tr::BLK + i * 1024), 16, goff[i], 0, 0,
+                                             kAuxNT);
+  }
+}
+
 // Online-softmax update with the page in a slot; the page holds at least one
 // key below k1, so the new running max is finite.
 template <int HD, bool F8>
@@ -1329,6 +1354,13 @@ __device__ __forceinline__ void prefill_item32(const uint16_t *__restrict__ qkv,
         *reinterpret_cast<u32x2_t *>(dst + ob * 32 + 8 * g) = w;
       }
   }
+}
+
+// One 16-byte-per-lane load from a buffer range straight into LDS: lane l
+// fills bytes 16 l .. 16 l + 15 from dst (wave-uniform) with the bytes at its
+// offset (zeros past the range).
+__device__ __forceinline__ void lds_dma16(buf_rsrc_t r, uint8_t *dst, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t *)dst, 16, off, 0, 0, 0);
 }
 
 // The 32x32 prefill item for bf16 caches with its tiles loaded straight
