@@ -19,7 +19,7 @@ constexpr float kNoScore = -__builtin_inff();
 struct AttendArgs {
   const uint16_t *qkv;
   uint16_t *out;
-  float *lse, *weights, *part_o, *part_ml, *scores;
+  float *lse, *weights, *part_o, *part_ml, *scores, *wparts;
   const int32_t *first_key;
   const float *slopes;
   KV kv;

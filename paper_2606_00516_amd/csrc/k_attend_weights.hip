@@ -6,7 +6,10 @@
 // weight is one lane's register sum and no atomics are needed.  A block takes
 // 64 keys of a (request, kv head), held by each of its four wavefronts as two
 // 32-key A operands; the wavefronts take every fourth run of 32 rows (32 / G
-// positions x G heads), loaded straight into registers one run ahead: no LDS
+// positions x G heads; with few blocks the runs are split into parts, which
+// k_attend_weights_join adds in their order; with many blocks and few runs each
+// wavefront has 64 keys of its own, by the plan's rule), loaded straight into
+// registers one run ahead: no LDS
 // and no barrier on the walk, whose length is that of the block whose keys
 // the most rows see (six prompts of about 1800 rows in documents of 300, hd 64:
 // 96 us through LDS tiles that the block shared, 56 so).  Per 32 x 64 scores 2 hd / 16 products of 32
@@ -22,7 +25,38 @@ namespace eb {
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = kWeightWaves;
+
+// A block's request, place in it and keys.
+struct WBlock {
+  int k, seq, row0, c, n, prefix, parts, at, part, j0, k0, keys;  // at: block of keys in the request
+};
+__device__ __forceinline__ WBlock weight_block(const AttendArgs &a, meta_t m, int blk, bool join) {
+  WBlock b;
+  b.k = last_at_or_below(m + (join ? PRE_WJOIN0 : PRE_WBLOCK0) * a.n, a.n, blk);
+  const auto field = [&](int f) { return __builtin_amdgcn_readfirstlane(m[f * a.n + b.k]); };
+  b.seq = field(PRE_SEQ);
+  b.row0 = field(PRE_ROW);
+  b.c = field(PRE_CTX);
+  b.n = field(PRE_LEN);
+  b.prefix = field(PRE_PREFIX);
+  b.parts = field(PRE_WPARTS);
+  const int local = blk - field(join ? PRE_WJOIN0 : PRE_WBLOCK0), parts = join ? 1 : max(b.parts, 1);
+  b.at = local / parts;
+  b.part = local - b.at * parts;
+  b.j0 = a.weight_rows > 0 ? max(0, b.n - a.weight_rows) : 0;
+  b.keys = b.parts == 0 ? kWeightKeys * kWaves : kWeightKeys;
+  b.k0 = (min(b.c, attend_first(b.c + b.j0, a.window)) / b.keys + b.at) * b.keys;
+  return b;
+}
+// The new weight of a key from what this call gives it.
+__device__ __forceinline__ void add_weight(const AttendArgs &a, const WBlock &b, int kh, int key, float got) {
+  if (key >= b.c + b.n) return;
+  const int phys = a.kv.bt[(size_t)b.seq * a.kv.max_pages + key / kPageSize];
+  if ((unsigned)phys >= (unsigned)a.kv.num_pages) return;
+  float *dst = a.weights + ((size_t)phys * a.nkv + kh) * kPageSize + key % kPageSize;
+  *dst = key < b.c ? *dst + got : got;  // a new key starts at what this call gives it
+}
 
 template <int HD, bool F8, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
@@ -32,21 +66,19 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
   const int lq = lane & 31, lh = lane >> 5;
   const meta_t m = meta_words(a);
   const int blk = blockIdx.x / a.nkv, kh = blockIdx.x - blk * a.nkv;
-  const int k = last_at_or_below(m + PRE_WBLOCK0 * a.n, a.n, blk);
-  const auto field = [&](int f) { return __builtin_amdgcn_readfirstlane(m[f * a.n + k]); };
-  const int seq = field(PRE_SEQ), row0 = field(PRE_ROW), c = field(PRE_CTX), n = field(PRE_LEN),
-            prefix = field(PRE_PREFIX);
+  const WBlock b = weight_block(a, m, blk, false);
+  const int seq = b.seq, row0 = b.row0, c = b.c, n = b.n, prefix = b.prefix, j0 = b.j0;
   const int klen = c + n, G = a.group, PB = 32 / G;  // positions per run
-  const int j0 = a.weight_rows > 0 ? max(0, n - a.weight_rows) : 0;
-  const int first = min(c, attend_first(c + j0, a.window)) / kWeightKeys;
-  const int k0 = (first + blk - field(PRE_WBLOCK0)) * kWeightKeys;  // the block's first key
+  const bool apart = b.parts == 0;                   // each wavefront has keys of its own
+  const int kb = b.k0, kend = kb + b.keys;           // the block's keys
+  const int k0 = kb + (apart ? wave * kWeightKeys : 0);
   const int cols = (a.nq + 2 * a.nkv) * HD;
 
   // rows that may see the block's keys: from the first position at or past
   // its first key (all of them below a prefix), up to the window's reach
-  int ja = k0 < prefix ? j0 : max(j0, k0 - c);
+  int ja = kb < prefix ? j0 : max(j0, kb - c);
   int jb = n;
-  if (a.window > 0) jb = min(n, max(0, k0 + kWeightKeys - 1 + a.window - c));
+  if (a.window > 0) jb = min(n, max(0, kend - 1 + a.window - c));
   if (a.first_key) {
     // documents: only rows from the first to the last that sees one of the
     // block's keys are worth their products
@@ -61,7 +93,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int ju = j + 256 * u;
-        if (ju < jb && f[u] < min(k0 + kWeightKeys, max(c + ju + 1, prefix))) {
+        if (ju < jb && f[u] < min(kend, max(c + ju + 1, prefix))) {
           mn = min(mn, ju);
           mx = max(mx, ju + 1);
         }
@@ -80,14 +112,21 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
     ja = max(ja, __builtin_amdgcn_readfirstlane(span[0]));
     jb = min(jb, __builtin_amdgcn_readfirstlane(span[1]));
   }
-  const int runs = ja < jb ? (jb - ja + PB - 1) / PB : 0;
+  int runs = ja < jb ? (jb - ja + PB - 1) / PB : 0;
+  if (b.parts > 1) {  // this part's runs
+    const int lo = (int)((int64_t)runs * b.part / b.parts), hi = (int)((int64_t)runs * (b.part + 1) / b.parts);
+    jb = min(jb, ja + hi * PB);
+    ja += lo * PB;
+    runs = hi - lo;
+  }
+  const int t0 = apart ? 0 : wave, step = apart ? 1 : kWaves;  // this wavefront's runs
 
   float acc[KG][16];
 #pragma unroll
   for (int g = 0; g < KG; ++g)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[g][i] = 0.f;
-  if (wave < runs) {
+  if (t0 < runs) {
     // K of the block's keys: lane (lq, lh) holds dims 16 ks + 8 lh .. of key 32 g + lq
     u32x4_t kf[KG][NKS];
 #pragma unroll
@@ -181,12 +220,12 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
       }
     };
     Run x, y;
-    load(wave, x);
-    for (int t = wave; t < runs; t += 2 * kWaves) {
-      load(t + kWaves, y);
+    load(t0, x);
+    for (int t = t0; t < runs; t += 2 * step) {
+      load(t + step, y);
       add(t, x);
-      load(t + 2 * kWaves, x);
-      add(t + kWaves, y);
+      load(t + 2 * step, x);
+      add(t + step, y);
     }
   }
   // Over the 32 rows' lanes by halves: in each exchange a lane keeps the half
@@ -209,19 +248,29 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
   }
   part[wave][32 * (lq >> 4) + 8 * ((lq >> 2) & 3) + 4 * lh + (lq & 3)] = v[0];
   __syncthreads();
-  if (tid < kWeightKeys) {
-    const int key = k0 + tid;
-    if (key < klen) {
-      const int phys = a.kv.bt[(size_t)seq * a.kv.max_pages + key / kPageSize];
-      if ((unsigned)phys < (unsigned)a.kv.num_pages) {
-        float got = part[0][tid];
+  if (apart) {
+    add_weight(a, b, kh, kb + tid, part[wave][lane]);
+  } else if (tid < kWeightKeys) {
+    float got = part[0][tid];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) got += part[w][tid];
-        float *dst = a.weights + ((size_t)phys * a.nkv + kh) * kPageSize + key % kPageSize;
-        *dst = key < c ? *dst + got : got;  // a new key starts at what this call gives it
-      }
-    }
+    for (int w = 1; w < kWaves; ++w) got += part[w][tid];
+    if (b.parts > 1)
+      a.wparts[((size_t)(m[PRE_WPART0 * a.n + b.k] + b.at * b.parts + b.part) * a.nkv + kh) * kWeightKeys + tid] = got;
+    else
+      add_weight(a, b, kh, kb + tid, got);
   }
+}
+
+// Joins the parts of the rows, in their order.
+__global__ __launch_bounds__(kWeightKeys) void k_attend_weights_join(AttendArgs a) {
+  const meta_t m = meta_words(a);
+  const int blk = blockIdx.x / a.nkv, kh = blockIdx.x - blk * a.nkv, tid = threadIdx.x;
+  const WBlock b = weight_block(a, m, blk, true);
+  const float *src =
+      a.wparts + ((size_t)(m[PRE_WPART0 * a.n + b.k] + b.at * b.parts) * a.nkv + kh) * kWeightKeys + tid;
+  float got = 0.f;
+  for (int p = 0; p < b.parts; ++p) got += src[(size_t)p * a.nkv * kWeightKeys];
+  add_weight(a, b, kh, b.k0 + tid, got);
 }
 
 }  // namespace
@@ -251,6 +300,9 @@ hipError_t launch_attend_weights(const Shape &s, const AttendCall &c, const Atte
       EB_WTS(64, false);
   }
 #undef EB_WTS
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || c.plan->pre_wjoins == 0) return e;
+  hipLaunchKernelGGL(k_attend_weights_join, dim3((unsigned)(c.plan->pre_wjoins * s.nkv)), dim3(kWeightKeys), 0, st, a);
   return hipGetLastError();
 }
 
@@ -281,6 +333,7 @@ hipError_t launch_attend(const Shape &s, const AttendCall &c, hipStream_t st) {
   a.part_o = reinterpret_cast<float *>(c.ws + p.o_part_o);
   a.part_ml = reinterpret_cast<float *>(c.ws + p.o_part_ml);
   a.scores = c.weights ? reinterpret_cast<float *>(c.ws + p.o_scores) : nullptr;
+  a.wparts = reinterpret_cast<float *>(c.ws + p.o_wparts);
   a.first_key = c.first_key;
   a.slopes = c.slopes;
   a.kv = c.kv;

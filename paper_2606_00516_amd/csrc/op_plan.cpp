@@ -21,6 +21,22 @@ int32_t chunk_splits(int32_t rows, int32_t kv_heads, int32_t q_blocks, int32_t t
   const int32_t least = rows > kAttendRows ? 16 : tiles > 40 ? 12 : 4;  // tiles per split
   return std::max(1, std::min((512 + items - 1) / items, tiles / least));
 }
+
+// Parts of the rows in the weights pass of a chunk of `runs` runs of 32 rows,
+// where the call has `blocks` blocks of 64 keys of a kv head.  Where these are
+// few, enough parts to fill the chip, of four runs a wavefront at least.  Where
+// they are many and the runs no more than a block's wavefronts, 0: each
+// wavefront takes all of them for 64 keys of its own.  (One prompt of 1009 rows,
+// 4 kv heads, 64 blocks: in 8 parts 21 us and 4.5 to join, whole 62; six prompts
+// of 1376 blocks: in 2 parts 14 us slower.  Eight requests of 2 or 3 rows over
+// 5000 keys, 2560 blocks: keys apart 22.6 us, not 28.3; three of 32 counted rows
+// and 480 blocks: 10.8 and 8.0.)
+// A row's own results do not depend on its batch; the order of a weight's sum
+// may.
+int32_t weight_parts(int32_t runs, int64_t blocks) {
+  if (runs <= kWeightWaves && blocks >= 1024) return 0;
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>((512 + blocks - 1) / blocks, runs / (4 * kWeightWaves)));
+}
 }  // namespace
 
 bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, const int32_t *prefix, bool weights,
@@ -39,7 +55,7 @@ bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   int64_t runs = 0;
   int32_t part = 0;  // partials of the chunks, behind those of the decode rows
   const auto fits = [&]() {  // (each request adds less than 2^30 to a count: looked at after each, none wraps)
-    return std::max({p.dec_splits, p.dec_wblocks, p.pre_tiles, p.pre_wblocks}) <= kMostBlocks / nkv &&
+    return std::max({p.dec_splits, p.dec_wblocks, p.pre_tiles, p.pre_wblocks, p.pre_wparts}) <= kMostBlocks / nkv &&
            part <= 0x3FFFFFFF && runs <= 0x7FFFFFFF;
   };
   // the longest splits first: the launch ends on the shortest
@@ -70,6 +86,14 @@ bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
     if (!fits()) return false;
   }
   std::stable_sort(many.begin(), many.end(), [&](int32_t x, int32_t y) { return keys_of(x) > keys_of(y); });
+  // blocks of so many keys of request i that the rows from j on may see
+  const auto key_blocks = [&](int i, int32_t j, int32_t keys) {
+    const int32_t c = b.context_lens_host[i];
+    return (c + b.chunk_lens_host[i] + keys - 1) / keys - std::min(c, attend_first(c + j, window)) / keys;
+  };
+  int64_t wblocks = 0;  // (all rows: the workspace's size does not know weight_rows)
+  if (weights)
+    for (int i : many) wblocks += (int64_t)key_blocks(i, 0, kWeightKeys) * nkv;
   p.n_pre = (int32_t)many.size();
   p.pre.assign((size_t)PRE_FIELDS * p.n_pre, 0);
   part = p.dec_splits;
@@ -106,8 +130,16 @@ bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
       // every new key gets its first value, every key that a counted row may
       // see gets its share
       const int32_t j0 = weight_rows > 0 ? std::max(0, n - weight_rows) : 0;
-      const int32_t first = std::min(c, attend_first(c + j0, window)) / kWeightKeys;
-      p.pre_wblocks += (c + n + kWeightKeys - 1) / kWeightKeys - first;
+      const int32_t parts = weight_parts((n - j0 + 32 / G - 1) / (32 / G), wblocks);
+      const int32_t wb = key_blocks(i, j0, parts == 0 ? kWeightKeys * kWeightWaves : kWeightKeys);
+      f[PRE_WPARTS * m] = parts;
+      f[PRE_WPART0 * m] = p.pre_wparts;
+      f[PRE_WJOIN0 * m] = p.pre_wjoins;
+      p.pre_wblocks += wb * std::max(1, parts);
+      if (parts > 1) {
+        p.pre_wparts += wb * parts;
+        p.pre_wjoins += wb;
+      }
     }
     if (!fits()) return false;
   }
@@ -123,6 +155,7 @@ bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   p.o_part_o = take((size_t)part * cfg.n_q_heads * cfg.head_dim * 4);
   p.o_part_ml = take((size_t)part * cfg.n_q_heads * 8);
   p.o_scores = take((size_t)runs * 64);
+  p.o_wparts = take((size_t)p.pre_wparts * nkv * kWeightKeys * 4);
   p.total = off;
   return true;
 }

@@ -11,7 +11,8 @@ namespace eb {
 
 constexpr int kAttendTile = 64;    // keys per step of a chunk's rows
 constexpr int kAttendRows = 128;   // query rows (positions x heads of the group) per block
-constexpr int kWeightKeys = 64;    // keys per block of the weights pass of a chunk
+constexpr int kWeightKeys = 64;    // keys per wavefront of the weights pass of a chunk
+constexpr int kWeightWaves = 4;    // wavefronts of its blocks
 constexpr int kWeightSpan = 1024;  // keys per block of the weights pass of a decode row
 
 // Keys per split of a decode row that sees `keys` of them: equal shares, a
@@ -41,21 +42,22 @@ struct AttendPlan {
   int32_t dec_most = 0;  // keys of the longest split
   bool dec_combine = false;
   std::vector<int32_t> dec;
-  int32_t n_pre = 0, pre_tiles = 0, pre_comb_rows = 0, pre_wblocks = 0;
+  int32_t n_pre = 0, pre_tiles = 0, pre_comb_rows = 0, pre_wblocks = 0, pre_wjoins = 0, pre_wparts = 0;
   std::vector<int32_t> pre;
   // byte offsets in the workspace (256-byte aligned)
-  size_t o_dec = 0, o_pre = 0, o_lse = 0, o_part_o = 0, o_part_ml = 0, o_scores = 0, total = 0;
+  size_t o_dec = 0, o_pre = 0, o_lse = 0, o_part_o = 0, o_part_ml = 0, o_scores = 0, o_wparts = 0, total = 0;
 };
 
 // request, row, context, first split, first block of the weights pass, first
 // 16-score run
 enum DecField { DEC_SEQ = 0, DEC_ROW, DEC_CTX, DEC_SPLIT0, DEC_WBLOCK0, DEC_SCORE0, DEC_FIELDS };
 // request, first row, context, rows, prefix, first tile, splits of the keys,
-// first partial, first row among those with several splits, first block of
-// the weights pass
+// first partial, first row among those with several splits; of the weights
+// pass the first block, the parts of the rows (0: each wavefront has keys of
+// its own), and for those with several the first partial and joining block
 enum PreField {
   PRE_SEQ = 0, PRE_ROW, PRE_CTX, PRE_LEN, PRE_PREFIX, PRE_TILE0, PRE_NSPLIT, PRE_PART0, PRE_COMB0, PRE_WBLOCK0,
-  PRE_FIELDS
+  PRE_WPARTS, PRE_WPART0, PRE_WJOIN0, PRE_FIELDS
 };
 
 // window 0: none; prefix: per request, or null.  The batch has passed

@@ -157,3 +157,45 @@ def test_nan_weights_of_any_sign_are_largest(lens):
         return torch.where(u < 6, bits[u.clamp(max=5)].view(torch.float32), w)
     E.run(R.shape(4, 2, 64), lens, [n // 10 for n in lens], 1, 2, make=make)
     E.run(R.shape(4, 2, 64), lens, [n // 3 for n in lens], 1, 2, make=make)
+
+
+@pytest.mark.parametrize("case", [
+    dict(ctx=[0], chk=[1009]),                                             # one prompt: its rows in parts
+    dict(ctx=[300, 64, 700], chk=[500, 3, 260], softcap=30.0),             # in parts, whole, in parts
+    dict(ctx=[2000, 130, 63], chk=[2, 4, 16], window=700),
+    dict(ctx=[100, 0, 900], chk=[600, 40, 3], weight_rows=32),
+    dict(ctx=[10, 250], chk=[700, 5], window=100, prefix=[400, 255]),
+])
+@pytest.mark.parametrize("heads,fp8", [((8, 1, 64), False), ((8, 1, 128), True), ((4, 4, 64), False)])
+def test_weights_of_rows_in_parts_and_keys_apart(heads, fp8, case):
+    sh, kw = R.shape(*heads), dict(case)
+    got, ref, _, _ = run(sh, kw.pop("ctx"), kw.pop("chk"), fp8=fp8, weights=True, **kw)
+    check(got, ref)
+
+
+@pytest.mark.parametrize("n", [3, 800])
+def test_weights_of_documents_in_parts(n):
+    sh, ctx, chk = R.shape(8, 1, 64), [40, 0], [n, 700]
+    first = np.concatenate([40 + np.arange(n) // 90 * 90, np.arange(700) // 130 * 130])
+    first[-60:] = 2 ** 30                                                  # padding rows
+    got, ref, _, _ = run(sh, ctx, chk, first=first, weights=True)
+    check(got, ref)
+    a = run(sh, ctx[1:], chk[1:], first=first[n:], weights=True)[0]
+    b = run(sh, ctx[1:], chk[1:], first=first[n:], weights=True)[0]
+    assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("heads,fp8", [((8, 8, 64), False), ((16, 8, 128), True), ((32, 8, 128), False)])
+@pytest.mark.parametrize("kw", [dict(), dict(weight_rows=2, softcap=20.0), dict(window=3000, prefix=[9003, 0, 64])])
+def test_weights_of_few_rows_over_many_keys(heads, fp8, kw):
+    # more than 1024 blocks of 64 keys and few rows: keys apart; the first request's keys end inside a wavefront's 64
+    sh, ctx, chk = R.shape(*heads), [9000, 700, 61], [3, 70, 5]
+    got, ref, _, _ = run(sh, ctx, chk, fp8=fp8, weights=True, **kw)
+    check(got, ref)
+
+
+def test_weights_of_few_rows_of_documents_over_many_keys():
+    sh, ctx, chk = R.shape(8, 8, 64), [9000, 63], [4, 3]
+    first = np.array([8000, 8990, 2 ** 30, 9003, 0, 50, 65])
+    got, ref, _, _ = run(sh, ctx, chk, first=first, weights=True)
+    check(got, ref)
