@@ -78,7 +78,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
   // its first key (all of them below a prefix), up to the window's reach
   int ja = kb < prefix ? j0 : max(j0, kb - c);
   int jb = n;
-  if (a.window > 0) jb = min(n, max(0, kend - 1 + a.window - c));
+  const int reach = kend - 1 - c;  // (compared before the window is added: any int32 is a window)
+  if (a.window > 0 && reach < n - a.window) jb = max(0, reach + a.window);
   if (a.first_key) {
     // documents: only rows from the first to the last that sees one of the
     // block's keys are worth their products
