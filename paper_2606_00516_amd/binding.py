@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from contextlib import nullcontext
 from typing import Optional
 
 import numpy as np
@@ -557,11 +558,12 @@ def _addr(a: np.ndarray) -> int:
 
 
 def _ws(ws: Optional[torch.Tensor], nbytes, stream, dev: int):
-    """(tensor to keep alive, address, bytes) of a workspace; allocated when None."""
+    """(tensor to keep alive, address, bytes) of a workspace; allocated when
+    None, from the pool of the stream that will write it: another stream's may
+    give out memory that kernels there are still to write."""
     if ws is None:
-        ws = alloc_workspace(nbytes())
-        if stream is not None:  # its memory is not given out again before that stream is done with it
-            ws.record_stream(stream)
+        with nullcontext() if stream is None else torch.cuda.stream(stream):
+            ws = alloc_workspace(nbytes())
     return ws, _dev(ws, torch.uint8, "ws", -1, dev), ws.numel()
 
 
@@ -633,9 +635,10 @@ def eb_op_attention_mod(h: Handle, qkv: torch.Tensor, kv: KvCache, batch: HostBa
     T, nq, dev = batch.c.num_tokens, h.n_q_heads, torch.cuda.current_device()
     p = _dev(qkv, torch.bfloat16, "qkv", T * h.qkv_cols, dev)
     if out is None:
-        out = torch.empty(T, nq * h.head_dim, dtype=torch.bfloat16, device=qkv.device)
-        if stream is not None:
-            out.record_stream(stream)
+        with nullcontext() if stream is None else torch.cuda.stream(stream):   # (as a workspace)
+            out = torch.empty(T, nq * h.head_dim, dtype=torch.bfloat16, device=qkv.device)
+        if stream is not None:   # the caller reads and drops it on the current one
+            out.record_stream(torch.cuda.current_stream())
     o = _dev(out, torch.bfloat16, "out", T * nq * h.head_dim, dev)
     z = None if lse is None else _dev(lse, torch.float32, "lse", T * nq, dev)
     w = None if kv_weights is None else _dev(kv_weights, torch.float32, "kv_weights", kv.num_pages * h.page_keys, dev)
