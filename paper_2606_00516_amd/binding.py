@@ -186,17 +186,25 @@ class HostBatch:
 def kv_struct(k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
               kv_scales=None) -> KvCache:
     """bf16 caches, or 8-bit E4M3 code caches (uint8 / float8_e4m3fn) with
-    kv_scales = (k_scale, v_scale)."""
+    kv_scales = (k_scale, v_scale).  The struct's `sizes` are what its pointers
+    do not carry: the tables' rows, the elements of a page (-1: not those of
+    keys and values alike), the device (-2: not one)."""
     assert block_tables.dtype == torch.int32 and block_tables.dim() == 2
     assert k_cache.dtype == v_cache.dtype
     if k_cache.dtype in _CODE_DTYPES:
         if kv_scales is None:
             raise ValueError("an 8-bit cache needs kv_scales = (k_scale, v_scale)")
-        return KvCache(_ptr(k_cache), _ptr(v_cache), int(k_cache.shape[0]), _ptr(block_tables),
-                       int(block_tables.shape[1]), KV_FP8_E4M3, float(kv_scales[0]), float(kv_scales[1]))
-    assert k_cache.dtype == torch.bfloat16
-    return KvCache(_ptr(k_cache), _ptr(v_cache), int(k_cache.shape[0]), _ptr(block_tables),
-                   int(block_tables.shape[1]), KV_BF16, 1.0, 1.0)
+        kv = KvCache(_ptr(k_cache), _ptr(v_cache), int(k_cache.shape[0]), _ptr(block_tables),
+                     int(block_tables.shape[1]), KV_FP8_E4M3, float(kv_scales[0]), float(kv_scales[1]))
+    else:
+        assert k_cache.dtype == torch.bfloat16
+        kv = KvCache(_ptr(k_cache), _ptr(v_cache), int(k_cache.shape[0]), _ptr(block_tables),
+                     int(block_tables.shape[1]), KV_BF16, 1.0, 1.0)
+    page = k_cache.numel() // max(1, kv.num_pages)
+    devices = {t.get_device() for t in (k_cache, v_cache, block_tables)}
+    kv.sizes = (int(block_tables.shape[0]), page if v_cache.numel() >= kv.num_pages * page else -1,
+                devices.pop() if len(devices) == 1 else -2)
+    return kv
 
 
 def weights_struct(w: dict) -> LayerWeights:
@@ -553,6 +561,20 @@ def _lens(a, name: str) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
+def _check_kv(h: Handle, kv: Optional[KvCache], num_seqs: int, dev: int):
+    """Compares what kv_struct noted of a cache with the call that reads it."""
+    sizes = getattr(kv, "sizes", None)   # (none in a struct filled by hand)
+    if sizes is None:
+        return
+    rows, page, device = sizes
+    if rows < num_seqs:
+        raise ValueError("block_tables needs a row per request")
+    if page != h.page_keys * h.head_dim:
+        raise ValueError("the cache must be [pages, n_kv, 16, head_dim] of the handle's shape, keys and values alike")
+    if device != dev:
+        raise ValueError("the cache and its block_tables must be on the current GPU")
+
+
 def _addr(a: np.ndarray) -> int:
     return a.__array_interface__["data"][0]
 
@@ -591,6 +613,11 @@ def eb_op_rotary_kv_append(h: Handle, rot: Rotary, qkv: torch.Tensor, kv: Option
     T, dev = batch.c.num_tokens, torch.cuda.current_device()
     p = _dev(qkv, torch.bfloat16, "qkv", T * h.qkv_cols, dev)
     pos = None if positions is None else _dev(positions, torch.int32, "positions", T, dev)
+    _check_kv(h, kv, batch.c.num_seqs, dev)
+    if h.cfg.qk_norm:
+        for t, name in zip(getattr(rot, "held", ()), ("q_norm", "k_norm")):   # (a struct filled by hand holds none)
+            if t is not None:
+                _dev(t, torch.bfloat16, name, h.head_dim, dev)
     held, wp, wn = _ws(ws, lambda: eb_op_rotary_kv_append_workspace_bytes(h, batch), stream, dev)
     _check(_lib.eb_op_rotary_kv_append(h.h, rot, p, kv, batch.c, pos, wp, wn, _raw_stream(stream, dev)))
     return qkv
@@ -607,14 +634,14 @@ def score_mod(scale: float = 0.0, softcap: float = 0.0, slopes: Optional[torch.T
     return m
 
 
-def _check_mod(h: Handle, batch: HostBatch, m: Optional[ScoreMod]):
+def _check_mod(h: Handle, batch: HostBatch, m: Optional[ScoreMod], dev: int = -1):
     if m is None:
         return None
     slopes, first, pre = getattr(m, "held", (None, None, None))   # (a struct filled by hand names its own addresses)
-    if slopes is not None and slopes.numel() != h.n_q_heads:
-        raise ValueError("slopes needs one value per query head")
-    if first is not None and first.numel() != batch.c.num_tokens:
-        raise ValueError("first_key needs one value per row")
+    if slopes is not None:   # one value per query head
+        _dev(slopes, torch.float32, "slopes", h.n_q_heads, dev)
+    if first is not None:    # one value per row
+        _dev(first, torch.int32, "first_key", batch.c.num_tokens, dev)
     if pre is not None and len(pre) != batch.c.num_seqs:
         raise ValueError("prefix_lens needs one value per request")
     return m
@@ -640,9 +667,10 @@ def eb_op_attention_mod(h: Handle, qkv: torch.Tensor, kv: KvCache, batch: HostBa
         if stream is not None:   # the caller reads and drops it on the current one
             out.record_stream(torch.cuda.current_stream())
     o = _dev(out, torch.bfloat16, "out", T * nq * h.head_dim, dev)
+    _check_kv(h, kv, batch.c.num_seqs, dev)
     z = None if lse is None else _dev(lse, torch.float32, "lse", T * nq, dev)
     w = None if kv_weights is None else _dev(kv_weights, torch.float32, "kv_weights", kv.num_pages * h.page_keys, dev)
-    m = _check_mod(h, batch, mod)
+    m = _check_mod(h, batch, mod, dev)
     held, wp, wn = _ws(ws, lambda: eb_op_attention_mod_workspace_bytes(h, batch, mod, w is not None), stream, dev)
     _check(_lib.eb_op_attention_mod(h.h, p, kv, batch.c, m, o, z, w, weight_rows, wp, wn, _raw_stream(stream, dev)))
     return out
@@ -664,6 +692,8 @@ def eb_op_kv_evict(h: Handle, src: KvCache, kv_weights: torch.Tensor, lens, keep
     if len(a) != len(b):
         raise ValueError("lens and keep_lens need one value per request each")
     dev = torch.cuda.current_device()
+    _check_kv(h, src, len(a), dev)
+    _check_kv(h, dst, len(a), dev)
     w = _dev(kv_weights, torch.float32, "kv_weights", src.num_pages * h.page_keys, dev)
     d = None if dst_weights is None else _dev(dst_weights, torch.float32, "dst_weights", dst.num_pages * h.page_keys, dev)
     k, stride = None, 0

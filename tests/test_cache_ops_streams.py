@@ -49,6 +49,7 @@ def world(monkeypatch):
     w.h = object.__new__(B.Handle)
     w.h.h = None
     w.h.n_q_heads, w.h.n_kv_heads, w.h.head_dim, w.h.qkv_cols, w.h.page_keys = 4, 2, 64, 512, 32
+    w.h.cfg = B.LayerConfig()
     w.kv = B.KvCache(256, 256, 4, 256, 4, 0, 1.0, 1.0)
     w.x = torch.zeros(1, 512, dtype=torch.bfloat16)
     w.weights = torch.zeros(4, 2, 16)
