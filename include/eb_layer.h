@@ -502,7 +502,8 @@ typedef struct eb_score_mod {
  * eb_op_attention with the scores and masks of mod; decode rows, chunks and
  * both together.  Keys and values that a row does not see do not reach it, not
  * even as infinities or NaN; pages that no row sees are not read.  A row that
- * sees nothing gets zeros.
+ * sees nothing gets zeros.  Sums are fp32: an output is finite while 2^32 times
+ * the sum of |v| over the row's visible keys is below fp32's largest value.
  * lse (fp32 [num_tokens, n_q] or NULL): ln of the sum of exp(s) over the
  * visible keys, -inf for a row that sees nothing.
  * kv_weights (or NULL): the weight each cached key has received, fp32

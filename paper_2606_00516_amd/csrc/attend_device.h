@@ -15,6 +15,12 @@
 namespace eb {
 
 constexpr float kNoScore = -__builtin_inff();
+// Room (log2 units) of a capped chunk row's probabilities above the 1 of an
+// ordinary softmax, without an eye on the row's maximum: scores to 22 in size.
+// A narrower one costs such rows, not others, 5 % (a look at every tile: 4096
+// rows over 32768 keys with scores to 20 in size, 16 units 2.68 ms, 32 units
+// 2.55); a wider one takes it from the values, whose sums share fp32's range.
+constexpr float kCappedSlack = 32.0f;
 
 struct AttendArgs {
   const uint16_t *qkv;
@@ -30,6 +36,7 @@ struct AttendArgs {
   // cap tanh(scale raw / cap) log2(e) = raw (tanh_c[0] + tanh_c[1] raw^2 + ..)
   // up to |raw| = small_raw (-1: the polynomial's coefficients leave fp32)
   float small_raw, tanh_c[5];
+  float even_raw;  // up to small_raw, and no score leaves +-kCappedSlack
   const int32_t *meta;
   Words inl;
 };
@@ -38,31 +45,32 @@ static_assert(sizeof(AttendArgs) < 4096, "kernel arguments");
 // One score from its raw product.  tanh(x) = 1 - 2 / (e^2x + 1), exact at
 // both ends (e^2x = 0 and infinite); its error of an ulp of 1 is below 1e-5
 // of a probability for caps of 100 and less.
-template <bool CAP>
-EB_DEV float mod_score(float raw, float qscale, float cap2) {
-  if constexpr (!CAP) return raw * qscale;
-  const float e = fast_exp2(raw * qscale);
-  return fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(e + 1.0f), cap2);
+EB_DEV float capped_score(float raw, const AttendArgs &a, float top) {  // top: the cap in log2 units, less any offset
+  const float e = fast_exp2(raw * a.qscale);
+  return fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(e + 1.0f), top);
 }
 
-// Whether every raw product of the wavefront is small beside the cap (|s| <=
-// 0.7 cap).  There tanh is its odd polynomial of degree 9 (minimax on that
-// range, off by 9.4e-8, less than the rounding of the other form): 6
-// full-rate operations a score and no transcendental, against 3 and 2 of a
-// quarter rate.
+// The largest size of a lane's raw products.  Where all of a wavefront's are
+// small beside the cap (|s| <= 0.7 cap: small_raw) tanh is its odd polynomial of
+// degree 9 (minimax on that range, off by 9.4e-8, less than the rounding of
+// the other form): 6 full-rate operations a score and no transcendental,
+// against 3 and 2 of a quarter rate.
 template <int N>
-EB_DEV bool all_small(const f32x16_t (&s)[N], const AttendArgs &a) {
+EB_DEV float largest(const f32x16_t (&s)[N]) {
   float big = 0.f;
 #pragma unroll
   for (int b = 0; b < N; ++b)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) big = fmaxf(fmaxf(fabsf(s[b][i]), fabsf(s[b][i + 1])), big);
-  return __builtin_amdgcn_ballot_w64(big > a.small_raw) == 0;
+  return big;
 }
-EB_DEV float small_score(float x, const AttendArgs &a) {
+EB_DEV bool none(bool x) { return __builtin_amdgcn_ballot_w64(x) == 0; }
+EB_DEV float small_ratio(float x, const AttendArgs &a) {
   const float u = x * x;
-  return x * fmaf(fmaf(fmaf(fmaf(a.tanh_c[4], u, a.tanh_c[3]), u, a.tanh_c[2]), u, a.tanh_c[1]), u, a.tanh_c[0]);
+  return fmaf(fmaf(fmaf(fmaf(a.tanh_c[4], u, a.tanh_c[3]), u, a.tanh_c[2]), u, a.tanh_c[1]), u, a.tanh_c[0]);
 }
+EB_DEV float small_score(float x, const AttendArgs &a) { return x * small_ratio(x, a); }
+EB_DEV float small_score(float x, const AttendArgs &a, float add) { return fmaf(x, small_ratio(x, a), add); }
 
 // First key the row at position p may see (the window and its own bound).
 EB_DEV int row_first(const AttendArgs &a, int row, int p) {

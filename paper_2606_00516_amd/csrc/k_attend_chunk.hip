@@ -48,11 +48,14 @@ __device__ __forceinline__ PreReq pre_req(const AttendArgs &a, meta_t m, int k) 
   return r;
 }
 
-// How scores are made.  kCapped (no bias, a cap up to kCappedMost) needs no
-// running maximum: |s| <= 92 in log2 units keeps 2^s and sums of 2^30 of them
-// inside fp32 and bf16 alike.
+// How scores are made.  kCapped (a cap, no bias) keeps no running maximum: a
+// row's probabilities are 2^(s - offset) with an offset of 0 as long as no
+// score of its block's tiles leaves +-kCappedSlack, which the largest of a
+// tile's products says (the cap's polynomial asks for it anyway).  Where one
+// does, the offset becomes the row's maximum if that is kCappedSlack above it,
+// or below -kCappedSlack at the row's first keys: probabilities stay below
+// 2^kCappedSlack and a row's largest above 2^-kCappedSlack, whatever the cap.
 enum Mode { kPlain = 0, kCapped, kBiased, kCapBiased };
-constexpr float kCappedMost = 64.0f;
 
 template <int HD, bool F8, int MODE>
 __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
@@ -274,6 +277,46 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
   if (t0 < t1) {
     if (tid < 2) odd[tid] = 0;
     f32x16_t sc[2];
+    // Looks over the products of tile t: whether all are small beside the cap,
+    // and whether they move the offset.
+    auto look = [&](int t, bool masked) {
+      const float big = largest<2>(sc);
+      bool small = none(big > (!FIXED ? a.small_raw : mrun < 0.f ? -1.f : a.even_raw));
+      if (FIXED && __builtin_expect(!small, 0)) {
+        small = none(big > a.small_raw);
+        // the row's largest score (the cap keeps their order) over its two lanes, and whether it had a key before
+        const int d = t * KT + 4 * lh - rlo;
+        const unsigned span = (unsigned)max(rhi - rlo, 0);
+        float top = kNoScore;
+        if (masked) {
+          asm volatile("");
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              top = fmaxf(top, (unsigned)(d + kb * 32 + 8 * (i >> 2) + (i & 3)) < span ? sc[kb][i] : kNoScore);
+        } else {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+        }
+        const auto tw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        const auto lw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lrun), __float_as_uint(lrun), false, false);
+        top = fmaxf(__uint_as_float(tw[0]), __uint_as_float(tw[1]));
+        const bool seen = top != kNoScore, first = lw[0] == 0u && lw[1] == 0u;
+        top = capped_score(top, a, a.cap2);
+        const bool move = seen && (top > mrun + kCappedSlack || (first && top < -kCappedSlack));
+        if (!none(move)) {
+          const float f = !move ? 1.f : first ? 0.f : fast_exp2(mrun - top);
+          lrun *= f;
+#pragma unroll
+          for (int ob = 0; ob < NOB; ++ob) oacc[ob] = oacc[ob] * f;
+          mrun = move ? top : mrun;
+        }
+      }
+      return small;
+    };
     const Ids i0 = page_ids(t0), i1 = page_ids(t0 + 1);
     Ids next = page_ids(t0 + 2);
     Ranges vat = ranges(t0 + 1, i1);
@@ -339,18 +382,19 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
       if constexpr (!LAST) scores(nxt, scn);
       __builtin_amdgcn_s_setprio(2);
       if constexpr (CAP) {
-        if (all_small<2>(sc, a)) {
+        if (look(t, masked)) {
           asm volatile("");  // (a branch: not both forms and a select)
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[kb][i] = small_score(sc[kb][i], a);
+            for (int i = 0; i < 16; ++i) sc[kb][i] = FIXED ? small_score(sc[kb][i], a, -mrun) : small_score(sc[kb][i], a);
         } else {
           asm volatile("");
+          const float top = FIXED ? a.cap2 - mrun : a.cap2;
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[kb][i] = mod_score<true>(sc[kb][i], a.qscale, a.cap2);
+            for (int i = 0; i < 16; ++i) sc[kb][i] = capped_score(sc[kb][i], a, top);
         }
       }
       if constexpr (BIAS) {
@@ -499,7 +543,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
           f32x4_t{oacc[ob][4 * g] * vscale, oacc[ob][4 * g + 1] * vscale, oacc[ob][4 * g + 2] * vscale,
                   oacc[ob][4 * g + 3] * vscale};
   if (lh == 0) {
-    a.part_ml[slot * 2] = mrun;
+    // (an offset where nothing was seen would count as a maximum where the splits are joined)
+    a.part_ml[slot * 2] = FIXED && l == 0.f ? kNoScore : mrun;
     a.part_ml[slot * 2 + 1] = l;
   }
 }
@@ -524,8 +569,7 @@ __global__ __launch_bounds__(256) void k_attend_chunk_combine(AttendArgs a) {
 hipError_t launch_attend_chunk(const Shape &s, const AttendCall &c, const AttendArgs &a, hipStream_t st) {
   const AttendPlan &p = *c.plan;
   const dim3 grid(p.pre_tiles * s.nkv);
-  const int mode = c.slopes ? (c.softcap > 0.f ? kCapBiased : kBiased)
-                            : (c.softcap > kCappedMost ? kCapBiased : c.softcap > 0.f ? kCapped : kPlain);
+  const int mode = c.slopes ? (c.softcap > 0.f ? kCapBiased : kBiased) : c.softcap > 0.f ? kCapped : kPlain;
 #define EB_CHUNK_M(HD_, F8_, MODE_)                                                        \
   case MODE_:                                                                              \
     hipLaunchKernelGGL((k_attend_chunk<HD_, F8_, MODE_>), grid, dim3(256), 0, st, a);      \

@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
     float s[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      s[j] = mod_score<CAP>(sa[j], a.qscale, a.cap2);
+      s[j] = CAP ? capped_score(sa[j], a, a.cap2) : sa[j] * a.qscale;
       if constexpr (BIAS) s[j] = fmaf(-slope, (float)(r.ctx - (kp + 4 * g + j)), s[j]);
     }
     const bool edge = kp + kPageSize > k1 || kp < lo;  // uniform

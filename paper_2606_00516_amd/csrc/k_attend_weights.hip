@@ -187,14 +187,14 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) s = mfma32x32x16(kf[g][ks], r.q[ks], s);
         if constexpr (CAP) {
-          if (all_small<1>(one, a)) {
+          if (none(largest<1>(one) > a.small_raw)) {
             asm volatile("");  // (a branch: not both forms and a select)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = small_score(s[i], a);
           } else {
             asm volatile("");
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = mod_score<true>(s[i], a.qscale, a.cap2);
+            for (int i = 0; i < 16; ++i) s[i] = capped_score(s[i], a, a.cap2);
           }
         }
         if constexpr (CAP || BIAS) {
@@ -356,6 +356,7 @@ hipError_t launch_attend(const Shape &s, const AttendCall &c, hipStream_t st) {
       ok = ok && std::fabs(a.tanh_c[i]) > 1e-36f && std::fabs(a.tanh_c[i]) < 1e36f;
     }
     a.small_raw = ok ? (float)(0.7 / y) : -1.f;  // (below every score: never)
+    a.even_raw = std::fmin(a.small_raw, (float)(kCappedSlack / (1.4426950408889634 * scale)));
   }
   hipError_t e = hipSuccess;
   if (p.n_dec > 0) {
