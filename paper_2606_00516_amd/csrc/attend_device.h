@@ -32,9 +32,9 @@ struct AttendArgs {
   int32_t nq, nkv, group, window, n, weight_rows;  // n: requests of the table
   int32_t stash;                                   // bytes of LDS for a decode split's scores; 0: stored as they come
   float qscale;                                    // no cap: to log2 units; cap: 2 log2(e) scale / cap
-  float cap2;                                      // cap in log2 units
+  float cap2, ratio;                               // cap in log2 units, scale / cap
   // cap tanh(scale raw / cap) log2(e) = raw (tanh_c[0] + tanh_c[1] raw^2 + ..)
-  // up to |raw| = small_raw (-1: the polynomial's coefficients leave fp32)
+  // up to |raw| = small_raw (-1: the coefficients leave fp32)
   float small_raw, tanh_c[5];
   float even_raw;  // up to small_raw, and no score leaves +-kCappedSlack
   const int32_t *meta;
@@ -42,19 +42,29 @@ struct AttendArgs {
 };
 static_assert(sizeof(AttendArgs) < 4096, "kernel arguments");
 
-// One score from its raw product.  tanh(x) = 1 - 2 / (e^2x + 1), exact at
-// both ends (e^2x = 0 and infinite); its error of an ulp of 1 is below 1e-5
-// of a probability for caps of 100 and less.
-EB_DEV float capped_score(float raw, const AttendArgs &a, float top) {  // top: the cap in log2 units, less any offset
+// tanh(x) = x P(x^2) to |x| = kTanhSmall, of degree 9: minimax of the relative
+// error on that range, 1.5e-7 (found by exchange in 64 bits).  Past it 1 - 2 /
+// (e^2x + 1), exact at both ends (e^2x = 0 and infinite), whose error is of the
+// same size there, but is that of the cap itself and not of a score far below
+// it: of caps of hundreds it would leave 1e-4.  Both hold a score to a few fp32
+// half steps of its own size.
+constexpr float kTanhSmall = 0.65f;
+constexpr double kTanhP[5] = {0.999999846, -0.333315002, 0.132978737, -0.0515179164, 0.0146250855};
+
+// One capped score from its raw product, any size of it; add: minus the offset.
+EB_DEV float capped_score(float raw, const AttendArgs &a, float add = 0.f) {
+  const float x = raw * a.ratio, u = x * x;
+  const float p = fmaf(fmaf(fmaf(fmaf((float)kTanhP[4], u, (float)kTanhP[3]), u, (float)kTanhP[2]), u, (float)kTanhP[1]),
+                       u, (float)kTanhP[0]);
   const float e = fast_exp2(raw * a.qscale);
-  return fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(e + 1.0f), top);
+  const float large = fmaf(-2.0f * a.cap2, __builtin_amdgcn_rcpf(e + 1.0f), a.cap2 + add);
+  return fabsf(x) <= kTanhSmall ? fmaf(a.cap2 * x, p, add) : large;
 }
 
 // The largest size of a lane's raw products.  Where all of a wavefront's are
-// small beside the cap (|s| <= 0.7 cap: small_raw) tanh is its odd polynomial of
-// degree 9 (minimax on that range, off by 9.4e-8, less than the rounding of
-// the other form): 6 full-rate operations a score and no transcendental,
-// against 3 and 2 of a quarter rate.
+// small (up to small_raw) the polynomial alone serves, the cap and the scale in
+// its coefficients: 6 full-rate operations a score and no transcendental,
+// against 13 and 2 of a quarter rate.
 template <int N>
 EB_DEV float largest(const f32x16_t (&s)[N]) {
   float big = 0.f;
@@ -65,12 +75,12 @@ EB_DEV float largest(const f32x16_t (&s)[N]) {
   return big;
 }
 EB_DEV bool none(bool x) { return __builtin_amdgcn_ballot_w64(x) == 0; }
-EB_DEV float small_ratio(float x, const AttendArgs &a) {
-  const float u = x * x;
+EB_DEV float small_ratio(float raw, const AttendArgs &a) {
+  const float u = raw * raw;
   return fmaf(fmaf(fmaf(fmaf(a.tanh_c[4], u, a.tanh_c[3]), u, a.tanh_c[2]), u, a.tanh_c[1]), u, a.tanh_c[0]);
 }
-EB_DEV float small_score(float x, const AttendArgs &a) { return x * small_ratio(x, a); }
-EB_DEV float small_score(float x, const AttendArgs &a, float add) { return fmaf(x, small_ratio(x, a), add); }
+EB_DEV float small_score(float raw, const AttendArgs &a) { return raw * small_ratio(raw, a); }
+EB_DEV float small_score(float raw, const AttendArgs &a, float add) { return fmaf(raw, small_ratio(raw, a), add); }
 
 // First key the row at position p may see (the window and its own bound).
 EB_DEV int row_first(const AttendArgs &a, int row, int p) {

@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
         const auto lw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lrun), __float_as_uint(lrun), false, false);
         top = fmaxf(__uint_as_float(tw[0]), __uint_as_float(tw[1]));
         const bool seen = top != kNoScore, first = lw[0] == 0u && lw[1] == 0u;
-        top = capped_score(top, a, a.cap2);
+        top = capped_score(top, a);
         const bool move = seen && (top > mrun + kCappedSlack || (first && top < -kCappedSlack));
         if (!none(move)) {
           const float f = !move ? 1.f : first ? 0.f : fast_exp2(mrun - top);
@@ -390,11 +390,10 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
             for (int i = 0; i < 16; ++i) sc[kb][i] = FIXED ? small_score(sc[kb][i], a, -mrun) : small_score(sc[kb][i], a);
         } else {
           asm volatile("");
-          const float top = FIXED ? a.cap2 - mrun : a.cap2;
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[kb][i] = capped_score(sc[kb][i], a, top);
+            for (int i = 0; i < 16; ++i) sc[kb][i] = capped_score(sc[kb][i], a, FIXED ? -mrun : 0.f);
         }
       }
       if constexpr (BIAS) {

@@ -141,9 +141,21 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) sa = mfma16x16x32(dims8(slot, ks), qb[ks], sa);
     float s[4];
+    if constexpr (CAP) {
+      const float big = fmaxf(fmaxf(fabsf(sa[0]), fabsf(sa[1])), fmaxf(fabsf(sa[2]), fabsf(sa[3])));
+      if (none(big > a.small_raw)) {
+        asm volatile("");  // (a branch: not both forms and a select)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = small_score(sa[j], a);
+      } else {
+        asm volatile("");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = capped_score(sa[j], a);
+      }
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      s[j] = CAP ? capped_score(sa[j], a, a.cap2) : sa[j] * a.qscale;
+      if constexpr (!CAP) s[j] = sa[j] * a.qscale;
       if constexpr (BIAS) s[j] = fmaf(-slope, (float)(r.ctx - (kp + 4 * g + j)), s[j]);
     }
     const bool edge = kp + kPageSize > k1 || kp < lo;  // uniform

@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_weights(AttendArgs a) {
           } else {
             asm volatile("");
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = capped_score(s[i], a, a.cap2);
+            for (int i = 0; i < 16; ++i) s[i] = capped_score(s[i], a);
           }
         }
         if constexpr (CAP || BIAS) {
@@ -346,16 +346,16 @@ hipError_t launch_attend(const Shape &s, const AttendCall &c, hipStream_t st) {
   const float scale = c.scale * (c.kv.f8 ? c.kv.ks : 1.f);
   a.qscale = c.softcap > 0.f ? 2.f * kLog2e * (scale / c.softcap) : kLog2e * scale;
   a.cap2 = c.softcap * kLog2e;
+  a.ratio = c.softcap > 0.f ? scale / c.softcap : 0.f;
   if (c.softcap > 0.f) {
-    constexpr double k[5] = {0.999998495, -0.333269731, 0.132574549, -0.0501952578, 0.0131941869};
     const double y = (double)scale / c.softcap;
     double f = (double)c.softcap * 1.4426950408889634 * y;
     bool ok = true;
     for (int i = 0; i < 5; ++i, f *= y * y) {
-      a.tanh_c[i] = (float)(f * k[i]);
+      a.tanh_c[i] = (float)(f * kTanhP[i]);
       ok = ok && std::fabs(a.tanh_c[i]) > 1e-36f && std::fabs(a.tanh_c[i]) < 1e36f;
     }
-    a.small_raw = ok ? (float)(0.7 / y) : -1.f;  // (below every score: never)
+    a.small_raw = ok ? (float)(kTanhSmall / y) : -1.f;  // (below every score: never)
     a.even_raw = std::fmin(a.small_raw, (float)(kCappedSlack / (1.4426950408889634 * scale)));
   }
   hipError_t e = hipSuccess;
