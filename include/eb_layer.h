@@ -480,7 +480,8 @@ eb_status eb_op_rotary_kv_append(eb_handle *h, const eb_rotary *rot, void *qkv, 
 
 /* Scores and masks of eb_op_attention_mod.  For the row at cache position p =
  * c_i + j of request i and the key at position t of the same request:
- *   s = scale * q.k                         (scale 0: 1 / sqrt(head_dim); else finite, > 0)
+ *   s = scale * q.k                         (scale 0: 1 / sqrt(head_dim); else finite, > 0, and with
+ *                                            the cache's k_scale, and that over softcap, 1e-37 to 5e37)
  *   s = softcap * tanh(s / softcap)         when softcap > 0 (at most 1000)
  *   s = s - slopes[head] * |p - t|          when slopes (device fp32 [n_q]) is given
  * and the key is visible iff

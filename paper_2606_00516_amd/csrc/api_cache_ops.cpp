@@ -287,8 +287,9 @@ eb_status eb_op_attention_mod(eb_handle *h, const void *qkv, const eb_kv_cache *
       c.first_key = mod->first_key;
       c.window = mod->window;
     }
-    const double unit = 2.0 * c.scale * c.kv.ks / (c.softcap > 0.f ? c.softcap : 1.0);
-    if (!(unit < 1e38)) return api_fail(EB_ERR_CONFIG, "scale (with the cache's scale, over softcap) leaves fp32");
+    const double by = (double)c.scale * c.kv.ks, unit = by / (c.softcap > 0.f ? c.softcap : 1.0);
+    if (!(std::min(by, unit) > 1e-37 && std::max(by, unit) < 5e37))
+      return api_fail(EB_ERR_CONFIG, "scale (with the cache's scale, over softcap) leaves fp32");
     c.plan = &p;
     c.ws = static_cast<char *>(ws);
     const hipError_t e = launch_attend(*v.shape, c, st);
