@@ -109,10 +109,10 @@ eb_status rotary_turns(const Shape &sh, const eb_rotary &r, RotaryCall &c) {
     b = std::min(std::ceil(index(low)), (double)R - 1.);
     b = std::max(b, a + 1e-3);
   }
-  const double step = std::exp(-2. / R * std::log(theta));
-  long double w = 1.L;  // theta^(-2t/R) by products in extended precision (64 of them: far below an fp64 step)
-  for (int t = 0; t < R / 2; ++t, w *= step) {
-    double v = (double)w;
+  double w[64];
+  rotary_frequencies(R, theta, w);
+  for (int t = 0; t < R / 2; ++t) {
+    double v = w[t];
     if (r.scaling == EB_ROTARY_LINEAR) v /= f;
     if (r.scaling == EB_ROTARY_WAVELENGTH) {
       const double turns = len * v / kTwoPi, mix = std::min(std::max((turns - low) / (high - low), 0.), 1.);

@@ -3,6 +3,7 @@
 #include "op_plan.h"
 
 #include <algorithm>
+#include <cmath>
 #include <numeric>
 
 namespace eb {
@@ -158,6 +159,12 @@ bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
   p.o_wparts = take((size_t)p.pre_wparts * nkv * kWeightKeys * 4);
   p.total = off;
   return true;
+}
+
+void rotary_frequencies(int R, double theta, double *w) {
+  const long double step = std::exp(-2.L / R * std::log((long double)theta));
+  long double v = 1.L;
+  for (int t = 0; t < R / 2; ++t, v *= step) w[t] = (double)v;
 }
 
 bool plan_evict(int32_t n_kv, int32_t S, const int32_t *lens, const int32_t *keep, EvictPlan &p) {

@@ -68,6 +68,11 @@ bool plan_attend(const eb_layer_config &cfg, const eb_batch &b, int32_t window, 
 // Blocks of a launch: their threads (up to 512 each) are counted in 32 bits.
 constexpr int64_t kMostBlocks = 0x7FFFFF;
 
+// w[t] = theta^(-2t/R), t < R / 2: by products of a step in extended precision
+// (64 bits: R / 2 <= 64 of them leave 2^-57, far below an fp64 half step of
+// 2^-53), rounded once.
+void rotary_frequencies(int R, double theta, double *w);
+
 // ---- eviction ----
 constexpr int kEvictFew = 512;         // keys of the longest request: one wavefront chooses
 constexpr int kEvictBlock = 16384;     // one block chooses; longer: segments
