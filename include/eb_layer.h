@@ -512,7 +512,10 @@ typedef struct eb_score_mod {
  * every cached key the softmax weights of the rows and of the heads of its
  * group; the keys of the new rows start at what this call gives them; other
  * slots keep theirs.  weight_rows > 0: only the last weight_rows rows of each
- * request count.  No atomics: the same call gives the same bits.
+ * request count.  No atomics: the same call gives the same bits, and each page
+ * must belong to one request of the call (requests that share prefix pages go
+ * into calls after one another, which add up; in one call one's share would be
+ * lost).
  * want_weights: whether kv_weights will be given. */
 size_t eb_op_attention_mod_workspace_bytes(const eb_handle *h, const eb_batch *batch, const eb_score_mod *mod,
                                            int32_t want_weights);

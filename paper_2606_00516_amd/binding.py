@@ -658,7 +658,8 @@ def eb_op_attention_mod(h: Handle, qkv: torch.Tensor, kv: KvCache, batch: HostBa
                         kv_weights: Optional[torch.Tensor] = None, weight_rows: int = 0,
                         ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention with modified scores and masks; out bf16 [T, n_q head_dim],
-    lse fp32 [T, n_q] and kv_weights fp32 [pages, n_kv, 16] where wanted."""
+    lse fp32 [T, n_q] and kv_weights fp32 [pages, n_kv, 16] where wanted (then
+    no two requests of the call may share a page)."""
     T, nq, dev = batch.c.num_tokens, h.n_q_heads, torch.cuda.current_device()
     p = _dev(qkv, torch.bfloat16, "qkv", T * h.qkv_cols, dev)
     if out is None:
