@@ -550,6 +550,12 @@ def _raw_stream(stream, dev: int):
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
+def _i32(n, name: str) -> int:
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name} does not fit 32 bits")
+    return int(n)
+
+
 def _lens(a, name: str) -> np.ndarray:
     a = np.asarray(a)
     if a.dtype == np.int32 and a.flags.c_contiguous and a.ndim == 1:
@@ -594,8 +600,8 @@ def rotary(theta: float, rotary_dim: int = 0, layout: str = "half", scaling: str
            q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None) -> Rotary:
     """The rotation of eb_op_rotary_kv_append (eb_rotary); zeros stand for
     the defaults the header gives."""
-    r = Rotary(int(rotary_dim), ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], float(theta), float(factor),
-               float(low), float(high), float(magnitude), int(original_len),
+    r = Rotary(_i32(rotary_dim, "rotary_dim"), ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], float(theta), float(factor),
+               float(low), float(high), float(magnitude), _i32(original_len, "original_len"),
                None if q_norm is None else _dev(q_norm, torch.bfloat16, "q_norm"),
                None if k_norm is None else _dev(k_norm, torch.bfloat16, "k_norm"))
     r.held = (q_norm, k_norm)
@@ -628,7 +634,7 @@ def score_mod(scale: float = 0.0, softcap: float = 0.0, slopes: Optional[torch.T
     """Scores and masks of eb_op_attention_mod (eb_score_mod)."""
     pre = None if prefix_lens is None else _lens(prefix_lens, "prefix_lens")
     m = ScoreMod(float(scale), float(softcap), None if slopes is None else _dev(slopes, torch.float32, "slopes"),
-                 int(window), None if pre is None else pre.ctypes.data,
+                 _i32(window, "window"), None if pre is None else pre.ctypes.data,
                  None if first_key is None else _dev(first_key, torch.int32, "first_key"))
     m.held = (slopes, first_key, pre)
     return m
@@ -673,7 +679,8 @@ def eb_op_attention_mod(h: Handle, qkv: torch.Tensor, kv: KvCache, batch: HostBa
     w = None if kv_weights is None else _dev(kv_weights, torch.float32, "kv_weights", kv.num_pages * h.page_keys, dev)
     m = _check_mod(h, batch, mod, dev)
     held, wp, wn = _ws(ws, lambda: eb_op_attention_mod_workspace_bytes(h, batch, mod, w is not None), stream, dev)
-    _check(_lib.eb_op_attention_mod(h.h, p, kv, batch.c, m, o, z, w, weight_rows, wp, wn, _raw_stream(stream, dev)))
+    _check(_lib.eb_op_attention_mod(h.h, p, kv, batch.c, m, o, z, w, _i32(weight_rows, "weight_rows"), wp, wn,
+                                    _raw_stream(stream, dev)))
     return out
 
 
@@ -703,8 +710,8 @@ def eb_op_kv_evict(h: Handle, src: KvCache, kv_weights: torch.Tensor, lens, keep
             raise ValueError("kept must be [requests, n_kv, keys]")
         k, stride = _dev(kept, torch.int32, "kept", -1, dev), kept.shape[2]
     held, wp, wn = _ws(ws, lambda: eb_op_kv_evict_workspace_bytes(h, a, b), stream, dev)
-    _check(_lib.eb_op_kv_evict(h.h, src, w, len(a), _addr(a), _addr(b), sink, recent, dst, d, k, stride, wp, wn,
-                               _raw_stream(stream, dev)))
+    _check(_lib.eb_op_kv_evict(h.h, src, w, len(a), _addr(a), _addr(b), _i32(sink, "sink"), _i32(recent, "recent"), dst, d, k,
+                               stride, wp, wn, _raw_stream(stream, dev)))
     return np.minimum(a, b)
 
 
