@@ -12,11 +12,13 @@ namespace {
 // Splits of the keys of a chunk: enough blocks to fill the chip if this were
 // its only request, each long enough that the partials (fp32 rows written and
 // read again) and the blocks' starts stay small beside the keys it reads.  Few
-// rows over few keys are a matter of latency and split finely (5 rows over 2000
-// keys: splits of at least 4 tiles 15 us, of 8 20, of 16 32); over more keys
-// they come in batches that fill the chip (24 requests of 3 to 9 rows over up to
-// 4096 keys: of 4 tiles 71 us, of 8 59, of 12 53, of 16 57).  Many rows: 16 tiles
-// (a chunk of 1000 without context 31 us, 42 with splits of 8; 24 and 32 like 16).
+// rows: splits of at least 4 tiles suit a request alone, of 12 batches that fill
+// the chip (with the join, 32 heads over 8, 4 / 12 tiles: one request of 5 rows
+// over 2500 keys 13.9 / 26.1 us, over 4096 16.3 / 26.6; 24 of them over 2000 62 /
+// 50, over 4096 112 / 88).  The line at 40 tiles gives short contexts to the one
+// and long ones to the other: past it a lone request pays 10 us, below it a full
+// batch 20 %.  Many rows: 16 tiles (a chunk of 1000 without context 31 us, 42 with
+// splits of 8; 24 and 32 like 16).
 int32_t chunk_splits(int32_t rows, int32_t kv_heads, int32_t q_blocks, int32_t tiles) {
   const int32_t items = q_blocks * kv_heads;
   const int32_t least = rows > kAttendRows ? 16 : tiles > 40 ? 12 : 4;  // tiles per split

@@ -18,11 +18,14 @@ constexpr int kWeightSpan = 1024;  // keys per block of the weights pass of a de
 // Keys per split of a decode row that sees `keys` of them: equal shares, a
 // multiple of 64 (a page for each of a block's wavefronts), of at most the
 // size below.  They follow from the request alone, so that its result does
-// not depend on the batch.  Few keys are split finely, for a row alone (1500
-// keys, splits of 128: 6.2 us and 5.1 to join them; of 256: 7.6 and 4.6, of
-// 512: 10.4 and 4.1), the larger splits of many keys cost less to start and
-// join (64 rows over 2350 keys: splits of 256 up to 16384 keys 122 us, of 512
-// 115 us; 13 rows over 69000: of 512 351 us and 35, of 1024 333 and 13).
+// not depend on the batch.  Splits of 128 suit a row alone, larger ones, which
+// cost less to start and join, rows in batches.  With the join, 32 heads over 8,
+// splits of 128 / 256 / 512: one row over 1500 keys 10.0 / 11.1 / 13.4 us, over
+// 2100 10.8 / 11.3 / 12.9, over 4000 11.6 / 11.6 / 13.6, over 16000 28.2 / 19.8 /
+// 18.6; 4 rows over 2100 18.6 / 15.4 / 14.3, 64 rows 135 / 106 / 96.  So between
+// 2048 and about 8000 keys a lone row pays 2 us for what batches gain.  From 32768
+// keys on 1024 (13 rows over 69000: of 512 351 us and 35 to join, of 1024 333
+// and 13).
 __host__ __device__ inline int32_t attend_split_keys(int32_t keys) {
   const int32_t most = keys <= 512 ? 64 : keys <= 2048 ? 128 : keys <= 32768 ? 512 : 1024;
   const int32_t n = (keys + most - 1) / most;
