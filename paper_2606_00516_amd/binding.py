@@ -178,9 +178,18 @@ class HostBatch:
     """Holds the host int32 length arrays alive for the duration of a call."""
 
     def __init__(self, context_lens, chunk_lens):
-        self.ctx = np.ascontiguousarray(context_lens, dtype=np.int32)
-        self.chk = np.ascontiguousarray(chunk_lens, dtype=np.int32)
+        self.ctx, self.chk = self._ints(context_lens), self._ints(chunk_lens)
         self.c = Batch(len(self.ctx), int(self.chk.sum()), self.ctx.ctypes.data, self.chk.ctypes.data)
+
+    @staticmethod
+    def _ints(a) -> np.ndarray:
+        a = np.ascontiguousarray(a)
+        if a.dtype == np.int32:
+            return a
+        b = a.astype(np.int32)
+        if a.dtype.kind in "iu" and (a.tobytes() != b.astype(a.dtype).tobytes() or (a.dtype == np.uint32 and (b < 0).any())):
+            raise ValueError("a request's length does not fit 32 bits")   # (numpy has cut it off)
+        return b
 
 
 def kv_struct(k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
