@@ -195,9 +195,10 @@ class HostBatch:
 def kv_struct(k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
               kv_scales=None) -> KvCache:
     """bf16 caches, or 8-bit E4M3 code caches (uint8 / float8_e4m3fn) with
-    kv_scales = (k_scale, v_scale).  The struct's `sizes` are what its pointers
-    do not carry: the tables' rows, the elements of a page (-1: not those of
-    keys and values alike), the device (-2: not one)."""
+    kv_scales = (k_scale, v_scale).  The struct holds on to the tensors; its
+    `sizes` are what its pointers do not carry: the tables' rows, the elements
+    of a page (-1: not those of keys and values alike), the device (-2: not
+    one)."""
     assert block_tables.dtype == torch.int32 and block_tables.dim() == 2
     assert k_cache.dtype == v_cache.dtype
     if k_cache.dtype in _CODE_DTYPES:
@@ -213,6 +214,7 @@ def kv_struct(k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.
     devices = {t.get_device() for t in (k_cache, v_cache, block_tables)}
     kv.sizes = (int(block_tables.shape[0]), page if v_cache.numel() >= kv.num_pages * page else -1,
                 devices.pop() if len(devices) == 1 else -2)
+    kv.held = (k_cache, v_cache, block_tables)
     return kv
 
 
@@ -537,8 +539,7 @@ def eb_op_gather_kv(h: Handle, k_cache, v_cache, block_tables, context_lens, chu
 # operators on the paged cache: rotary append, modified attention, eviction.
 # They take the structs that a program keeps between calls: kv_struct(..) of
 # its cache and HostBatch(..) of the request lengths.  Structs made here hold
-# on to the tensors they point to; a kv_struct's cache and tables are the
-# caller's to keep.
+# on to the tensors they point to.
 # ---------------------------------------------------------------------------
 
 def _dev(t: torch.Tensor, dtype, name: str, numel: int = -1, dev: int = -1):
