@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-from contextlib import nullcontext
 from typing import Optional
 
 import numpy as np
@@ -303,6 +302,23 @@ def alloc_workspace(nbytes: int, device="cuda") -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+def _own(stream, make, returned: bool = True):
+    """Memory that a call makes itself, from the pool of the stream that will
+    write it: another stream's may give out memory that kernels there are still
+    to write.  What is returned is read and dropped on the current stream."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    if returned:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
+def _own_ws(stream, nbytes: int, device="cuda") -> torch.Tensor:
+    return _own(stream, lambda: alloc_workspace(nbytes, device), False)
+
+
 def _step(name, h: Handle, weights: dict, k_cache, v_cache, block_tables, context_lens, chunk_lens,
           x: torch.Tensor, y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None,
           kv_scales=None):
@@ -310,9 +326,9 @@ def _step(name, h: Handle, weights: dict, k_cache, v_cache, block_tables, contex
     mode = {"eb_layer_step_decode": "decode", "eb_layer_step_prefill": "prefill",
             "eb_layer_step_mixed": "mixed"}[name]
     if y is None:
-        y = torch.empty_like(x)
+        y = _own(stream, lambda: torch.empty_like(x))
     if ws is None:
-        ws = alloc_workspace(lib().eb_workspace_bytes(h.h, ctypes.byref(hb.c), MODES[mode]), x.device)
+        ws = _own_ws(stream, lib().eb_workspace_bytes(h.h, ctypes.byref(hb.c), MODES[mode]), x.device)
     kv = kv_struct(k_cache, v_cache, block_tables, kv_scales)
     w = weights_struct(weights)
     _check(getattr(lib(), name)(h.h, ctypes.byref(w), ctypes.byref(kv), ctypes.byref(hb.c), _ptr(x), _ptr(y),
@@ -348,7 +364,7 @@ def eb_layer_step_mixed_noalloc(h, weights, k_cache, v_cache, block_tables, cont
     y must be given by callers that cannot allocate)."""
     hb = HostBatch(context_lens, chunk_lens)
     if y is None:
-        y = torch.empty_like(x)
+        y = _own(stream, lambda: torch.empty_like(x))
     kv = kv_struct(k_cache, v_cache, block_tables, kv_scales)
     w = weights_struct(weights)
     _check(lib().eb_layer_step_mixed_noalloc(h.h, ctypes.byref(w), ctypes.byref(kv), ctypes.byref(hb.c), _ptr(x),
@@ -371,9 +387,9 @@ def eb_stack_step(h: Handle, mode: str, weights: list, caches: list, context_len
         raise ValueError("one cache entry per layer")
     hb = HostBatch(context_lens, chunk_lens)
     if y is None:
-        y = torch.empty_like(x)
+        y = _own(stream, lambda: torch.empty_like(x))
     if ws is None:
-        ws = alloc_workspace(lib().eb_stack_workspace_bytes(h.h, ctypes.byref(hb.c), MODES[mode]), x.device)
+        ws = _own_ws(stream, lib().eb_stack_workspace_bytes(h.h, ctypes.byref(hb.c), MODES[mode]), x.device)
     ws_arr = (LayerWeights * n)(*[weights_struct(w) for w in weights])
     kv_arr = (KvCache * n)(*[kv_struct(*c) for c in caches])
     _check(lib().eb_stack_step(h.h, MODES[mode], n, ws_arr, kv_arr, ctypes.byref(hb.c), _ptr(x), _ptr(y), _ptr(ws),
@@ -400,7 +416,7 @@ def eb_status_str(status: int) -> str:
 
 
 def eb_op_rmsnorm(h: Handle, x: torch.Tensor, gamma: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None):
-    out = torch.empty_like(x) if out is None else out
+    out = _own(stream, lambda: torch.empty_like(x)) if out is None else out
     _check(lib().eb_op_rmsnorm(h.h, _ptr(x), _ptr(gamma), _ptr(out), int(x.shape[0]), _stream(stream)))
     return out
 
@@ -410,9 +426,10 @@ def eb_op_gemm(A: torch.Tensor, W: torch.Tensor, epilogue: str = "store", residu
     M, K = A.shape
     N = W.shape[0]
     ncol = N // 2 if epilogue == "silu_mul" else N
-    out = torch.empty(M, ncol, dtype=torch.bfloat16, device=A.device) if out is None else out
+    if out is None:
+        out = _own(stream, lambda: torch.empty(M, ncol, dtype=torch.bfloat16, device=A.device))
     nb = int(lib().eb_op_gemm_workspace_bytes(M, N, K))
-    ws = alloc_workspace(nb, A.device)
+    ws = _own_ws(stream, nb, A.device)
     _check(lib().eb_op_gemm(_ptr(A), _ptr(W), _ptr(out), _ptr(residual), M, N, K, EPILOGUES[epilogue], _ptr(ws),
                             ws.numel(), _stream(stream)))
     return out
@@ -428,7 +445,8 @@ def eb_pack_weight(W: torch.Tensor, out: Optional[torch.Tensor] = None, stream=N
     if W.dtype != torch.bfloat16 or W.dim() != 2:
         raise ValueError("W must be a 2-D bf16 tensor")
     rows, cols = W.shape
-    out = torch.empty(rows * cols, dtype=torch.bfloat16, device=W.device) if out is None else out
+    if out is None:
+        out = _own(stream, lambda: torch.empty(rows * cols, dtype=torch.bfloat16, device=W.device))
     if out.numel() * 2 < eb_packed_weight_bytes(rows, cols):
         raise ValueError("out is smaller than the packed copy")
     _check(lib().eb_pack_weight(_ptr(W), _ptr(out), rows, cols, _stream(stream)))
@@ -458,9 +476,10 @@ def eb_op_gemm_w8(A: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor, epilo
     if w_scale.numel() != N:
         raise ValueError("w_scale needs one scale per row of W")
     ncol = N // 2 if epilogue == "silu_mul" else N
-    out = torch.empty(M, ncol, dtype=torch.bfloat16, device=A.device) if out is None else out
+    if out is None:
+        out = _own(stream, lambda: torch.empty(M, ncol, dtype=torch.bfloat16, device=A.device))
     nb = int(lib().eb_op_gemm_workspace_bytes(M, N, K))
-    ws = alloc_workspace(nb, A.device)
+    ws = _own_ws(stream, nb, A.device)
     _check(lib().eb_op_gemm_w8(_ptr(A), _ptr(W), _ptr(w_scale), _ptr(out), _ptr(residual), M, N, K,
                                EPILOGUES[epilogue], _ptr(ws), ws.numel(), _stream(stream)))
     return out
@@ -481,25 +500,26 @@ def eb_op_moe_ffn(b: torch.Tensor, w_router: torch.Tensor, w_gate_up: torch.Tens
     F = w_gate_up.shape[1] // 2
     if w_router.shape != (E, d) or w_gate_up.shape != (E, 2 * F, d) or w_down.shape != (E, d, F):
         raise ValueError("MoE weight shapes do not match")
-    out = torch.empty(T, d, dtype=torch.bfloat16, device=b.device) if out is None else out
-    ids = torch.empty(T, top_k, dtype=torch.int32, device=b.device) if return_routing else None
-    wts = torch.empty(T, top_k, dtype=torch.float32, device=b.device) if return_routing else None
+    make = lambda n, dtype: _own(stream, lambda: torch.empty(T, n, dtype=dtype, device=b.device))  # noqa: E731
+    out = make(d, torch.bfloat16) if out is None else out
+    ids = make(top_k, torch.int32) if return_routing else None
+    wts = make(top_k, torch.float32) if return_routing else None
     if ws is None:
-        ws = alloc_workspace(int(lib().eb_op_moe_ffn_workspace_bytes(T, d, E, top_k, F)), b.device)
+        ws = _own_ws(stream, int(lib().eb_op_moe_ffn_workspace_bytes(T, d, E, top_k, F)), b.device)
     _check(lib().eb_op_moe_ffn(_ptr(b), _ptr(residual), _ptr(w_router), _ptr(w_gate_up), _ptr(w_down), T, d, E,
                                int(top_k), F, 1 if renormalize else 0, _ptr(out), _ptr(ids), _ptr(wts), _ptr(ws),
                                ws.numel(), _stream(stream)))
     return (out, ids, wts) if return_routing else out
 
 
-def _op_ws(h, hb, mode="mixed", device="cuda"):
-    return alloc_workspace(lib().eb_workspace_bytes(h.h, ctypes.byref(hb.c), MODES[mode]), device)
+def _op_ws(h, hb, mode="mixed", device="cuda", stream=None):
+    return _own_ws(stream, lib().eb_workspace_bytes(h.h, ctypes.byref(hb.c), MODES[mode]), device)
 
 
 def eb_op_rope_kv_append(h: Handle, qkv: torch.Tensor, k_cache, v_cache, block_tables, context_lens, chunk_lens,
                          stream=None, kv_scales=None):
     hb = HostBatch(context_lens, chunk_lens)
-    ws = _op_ws(h, hb, device=qkv.device)
+    ws = _op_ws(h, hb, device=qkv.device, stream=stream)
     kv = kv_struct(k_cache, v_cache, block_tables, kv_scales)
     _check(lib().eb_op_rope_kv_append(h.h, _ptr(qkv), ctypes.byref(kv), ctypes.byref(hb.c), _ptr(ws), ws.numel(),
                                       _stream(stream)))
@@ -511,8 +531,9 @@ def eb_op_attention(h: Handle, qkv: torch.Tensor, k_cache, v_cache, block_tables
     hb = HostBatch(context_lens, chunk_lens)
     s = h.shape
     T = int(hb.chk.sum())
-    out = torch.empty(T, s.n_q_heads * s.head_dim, dtype=torch.bfloat16, device=qkv.device) if out is None else out
-    ws = _op_ws(h, hb, mode if mode in MODES else "mixed", qkv.device)
+    if out is None:
+        out = _own(stream, lambda: torch.empty(T, s.n_q_heads * s.head_dim, dtype=torch.bfloat16, device=qkv.device))
+    ws = _op_ws(h, hb, mode if mode in MODES else "mixed", qkv.device, stream)
     kv = kv_struct(k_cache, v_cache, block_tables, kv_scales)
     _check(lib().eb_op_attention(h.h, _ptr(qkv), ctypes.byref(kv), ctypes.byref(hb.c), _ptr(out), _ptr(ws),
                                  ws.numel(), MODES[mode], _stream(stream)))
@@ -526,9 +547,9 @@ def eb_op_gather_kv(h: Handle, k_cache, v_cache, block_tables, context_lens, chu
     hb = HostBatch(context_lens, chunk_lens)
     s = h.shape
     total = int((hb.ctx.astype(np.int64) + hb.chk).sum())
-    ok = torch.empty(total, s.n_kv_heads, s.head_dim, dtype=k_cache.dtype, device=k_cache.device)
-    ov = torch.empty_like(ok)
-    ws = _op_ws(h, hb, device=k_cache.device)
+    make = lambda: torch.empty(total, s.n_kv_heads, s.head_dim, dtype=k_cache.dtype, device=k_cache.device)  # noqa: E731
+    ok, ov = _own(stream, make), _own(stream, make)
+    ws = _op_ws(h, hb, device=k_cache.device, stream=stream)
     kv = kv_struct(k_cache, v_cache, block_tables, kv_scales if kv_scales is not None else (1.0, 1.0))
     _check(lib().eb_op_gather_kv(h.h, ctypes.byref(kv), ctypes.byref(hb.c), _ptr(ok), _ptr(ov), _ptr(ws), ws.numel(),
                                  _stream(stream)))
@@ -597,11 +618,9 @@ def _addr(a: np.ndarray) -> int:
 
 def _ws(ws: Optional[torch.Tensor], nbytes, stream, dev: int):
     """(tensor to keep alive, address, bytes) of a workspace; allocated when
-    None, from the pool of the stream that will write it: another stream's may
-    give out memory that kernels there are still to write."""
+    None."""
     if ws is None:
-        with nullcontext() if stream is None else torch.cuda.stream(stream):
-            ws = alloc_workspace(nbytes())
+        ws = _own(stream, lambda: alloc_workspace(nbytes()), False)
     return ws, _dev(ws, torch.uint8, "ws", -1, dev), ws.numel()
 
 
@@ -679,10 +698,7 @@ def eb_op_attention_mod(h: Handle, qkv: torch.Tensor, kv: KvCache, batch: HostBa
     T, nq, dev = batch.c.num_tokens, h.n_q_heads, torch.cuda.current_device()
     p = _dev(qkv, torch.bfloat16, "qkv", T * h.qkv_cols, dev)
     if out is None:
-        with nullcontext() if stream is None else torch.cuda.stream(stream):   # (as a workspace)
-            out = torch.empty(T, nq * h.head_dim, dtype=torch.bfloat16, device=qkv.device)
-        if stream is not None:   # the caller reads and drops it on the current one
-            out.record_stream(torch.cuda.current_stream())
+        out = _own(stream, lambda: torch.empty(T, nq * h.head_dim, dtype=torch.bfloat16, device=qkv.device))
     o = _dev(out, torch.bfloat16, "out", T * nq * h.head_dim, dev)
     _check_kv(h, kv, batch.c.num_seqs, dev)
     z = None if lse is None else _dev(lse, torch.float32, "lse", T * nq, dev)
