@@ -434,7 +434,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_chunk(AttendArgs a) {
           const float p0 = fast_exp2(RAW ? fmaf(s0, a.qscale, neg) : FIXED ? s0 : s0 + neg);
           const float p1 = fast_exp2(RAW ? fmaf(s1, a.qscale, neg) : FIXED ? s1 : s1 + neg);
           // P enters its product rounded to bf16 (half a step, 2^-8 of a
-          // probability); the sum keeps the fp32 values
+          // probability): the product takes bf16 alone, and P in two terms would
+          // be two products.  The sum keeps the fp32 values
           pk[kb][pr] = pack_bf16x2(p0, p1);
           l += p0 + p1;
         }

@@ -178,7 +178,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_decode(AttendArgs a) {
     lsum = lsum * alpha + ((pr[0] + pr[1]) + (pr[2] + pr[3]));
     mrun = mnew;
     // P^T as the B operand of the 16x16x16 product, rounded to bf16 (half a
-    // step, 2^-8 of a probability); the sum above keeps the fp32 values
+    // step, 2^-8 of a probability): it takes bf16 alone, and P in two terms would
+    // be two products.  The sum above keeps the fp32 values
     const u32x2_t pt = {pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3])};
     u32x2_t keep = {0xFFFFFFFFu, 0xFFFFFFFFu};  // values of masked tokens do not enter (0 x NaN)
     if (edge) {
