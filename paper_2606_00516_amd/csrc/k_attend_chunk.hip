@@ -13,8 +13,8 @@
 // size 128) 32 products of 32 cycles, 1024 cycles, stand against 32 scores per
 // lane: some 45 cycles of vector work each, 1440, where the cap's polynomial
 // serves: the vector unit bounds capped attention.  4096 rows over 32768 keys,
-// 32 heads: 2.65 to 2.83 ms by the box, 880 to 825 TFLOP/s; the counters put the
-// matrix cores at 45 % and the vector unit at 69 %, in part one after the other.
+// 32 heads: 2.58 to 2.9 ms by the box, 905 to 805 TFLOP/s; the counters put the
+// matrix cores at 41 % and the vector unit at 66 %, in part one after the other.
 //
 // With few rows the keys are split over blocks (the plan's rule) and joined by
 // k_attend_chunk_combine.
